@@ -389,8 +389,99 @@ int tss_get_attn_split(tss_ctx* ctx, int32_t* n_items, int32_t* groups, int32_t*
  * No passage of the paper. */
 int tss_check_kv(tss_ctx* ctx);
 
+/* ---- Operators on the caller's tensors -------------------------------------
+ *
+ * The operators below take device memory of the caller and no context: they
+ * check their host arguments (TSS_EINVAL, TSS_ENOSPACE; message from
+ * tss_last_error(NULL)), enqueue their launches on hip_stream, whose device
+ * must be the current one, and return without waiting.  They keep nothing
+ * between calls, allocate nothing and may be captured into a graph.  Calls that
+ * may run at the same time need workspaces of their own. */
+
+/* Element types of the operators' tensors. */
+enum tss_tensor_type { TSS_T_F32 = 0, TSS_T_BF16 = 1, TSS_T_F16 = 2 };
+
+#define TSS_LOGPROBS_MAX_TOKENS 8
+#define TSS_LOGPROBS_MAX_TOP 32
+
+/* Log probabilities of given tokens, the entropy and the most likely
+ * alternatives of each row of logits, in one pass over them.
+ *   logits: [rows][vocab] elements of `type`, rows row_stride elements apart
+ *     (row_stride >= vocab); aligned to one element.
+ *   tokens: [rows][n_tokens] given tokens, 0 <= n_tokens <= 8 (NULL for 0).
+ *   logprob, rank: [rows][n_tokens].  logprob = x[token] - ln sum e^x.  rank =
+ *     how many tokens come before it, larger logits first, the lower index
+ *     among equal ones (0: the greedy token).  A token outside [0, vocab), a
+ *     pad for instance, gets logprob NaN and rank -1.
+ *   entropy: [rows], in nats.
+ *   top_logprob, top_token: [rows][top_k], the first top_k tokens in that
+ *     order, 0 <= top_k <= min(32, vocab).
+ * Output pointers may be NULL (not wanted).  All arithmetic is in fp32.  A
+ * logit of -inf has probability 0; a row of nothing else gets logprobs of -inf
+ * and entropy 0.  NaN orders as the largest logit; a row that holds NaN or
+ * +inf gets NaN logprobs and entropy, its ranks and alternatives as ordered.
+ *   workspace: tss_token_logprobs_bytes() bytes of device memory, aligned to
+ *     16 (0 bytes: may be NULL); contents are of no meaning before and after.
+ * rows = 0 is allowed and launches nothing.  Paper: Algorithm 1 (the downstream
+ * metric of a task whose answer is the most probable of several). */
+size_t tss_token_logprobs_bytes(int32_t rows, int32_t vocab, int32_t n_tokens, int32_t top_k);
+int tss_token_logprobs(void* hip_stream, const void* logits, int32_t type, int64_t row_stride, int32_t rows,
+                       int32_t vocab, const int32_t* tokens, int32_t n_tokens, int32_t top_k, float* logprob,
+                       int32_t* rank, float* entropy, float* top_logprob, int32_t* top_token, void* workspace,
+                       size_t workspace_bytes);
+
+/* A paged KV cache as tss_kv_alloc lays its pages out: 16-token pages; for
+ * (layer, page) K of every head, then V of every head, 16 * head_dim elements
+ * each, K as [16][head_dim] and V as [4][head_dim][4] (token t of the page at
+ * [t / 4][:][t % 4]).  Pages are aligned to 16 bytes. */
+typedef struct {
+  void* pages;                /* [n_layers][n_pages][2][n_kv_heads][16 * head_dim] */
+  const int32_t* page_table;  /* device, [n_seqs][table_stride] page ids; unused by tss_copy_pages */
+  int32_t n_layers, n_pages, n_kv_heads, head_dim;  /* head_dim 64 or 128 */
+  int32_t type;               /* TSS_T_F32 or TSS_T_F16 */
+  int32_t n_seqs, table_stride;
+} tss_paged_kv;
+
+/* Attention of one layer over the cache with a sliding window and a few first
+ * tokens ("sinks") that stay visible.  Sequence s has lengths[s] tokens in the
+ * cache; the last of them are its queries, rows row_offsets[s] ..
+ * row_offsets[s + 1] - 1 of q and out, so row i of a sequence of r rows is
+ * the token at position p = lengths[s] - r + i.  It sees token t when t <= p and
+ * (t < sinks or t > p - window); window 0 sees every t <= p.
+ *   q, out: [rows][n_q_heads][head_dim] of the cache's type, rows q_stride /
+ *     out_stride elements apart (multiples of 8), aligned to 16 bytes; n_q_heads
+ *     is a multiple of n_kv_heads, query head h reads kv head
+ *     h / (n_q_heads / n_kv_heads).  out may be q.
+ *   row_offsets [n_seqs + 1] (increasing from 0), lengths [n_seqs]: device.
+ *   max_rows, max_length: upper bounds of a sequence's rows and length; rows
+ *     beyond max_rows are not computed.  Lengths beyond the page table or
+ *     max_length count as that many tokens.
+ *   scale: factor of q k, 0 for 1 / sqrt(head_dim).
+ * Rows behind the last sequence are left as they were.  A row that sees nothing
+ * (p < 0) gets zeros.  Slots that no row sees, and slots of page ids outside the
+ * pool, may hold anything; V that some rows see has to be finite for rows of the
+ * same sequence that do not.  fp16: operands and probabilities of the products
+ * in fp16, sums and softmax in fp32, one rounding to fp16 at the end; fp32:
+ * everything in fp32.
+ *   workspace: tss_window_attn_bytes() bytes for the same arguments, aligned
+ *     to 16 (0 bytes: may be NULL).
+ * Paper: Problem Formulation (verification against the cached prefix). */
+size_t tss_window_attn_bytes(const tss_paged_kv* kv, int32_t n_q_heads, int32_t rows, int32_t max_rows,
+                             int32_t max_length, int32_t sinks, int32_t window);
+int tss_window_attn(void* hip_stream, const tss_paged_kv* kv, int32_t layer, const void* q, int64_t q_stride,
+                    int32_t n_q_heads, const int32_t* row_offsets, const int32_t* lengths, int32_t rows,
+                    int32_t max_rows, int32_t max_length, int32_t sinks, int32_t window, float scale, void* out,
+                    int64_t out_stride, void* workspace, size_t workspace_bytes);
+
+/* Copies pages of the cache, in every layer: page dst[i] becomes page src[i]
+ * for i < n (host arrays, read during the call).  A page may be the source of
+ * several copies; a destination must appear once and be no source (TSS_EINVAL
+ * otherwise), so the copies have no order.  n = 0 launches nothing.  Paper:
+ * Problem Formulation (the cached prefix that several continuations share). */
+int tss_copy_pages(void* hip_stream, const tss_paged_kv* kv, const int32_t* src, const int32_t* dst, int32_t n);
+
 /* Message of the context's last failure; with ctx = NULL, of the calling
- * thread's last failed tss_create. */
+ * thread's last failed tss_create or operator call. */
 const char* tss_last_error(const tss_ctx* ctx);
 const char* tss_status_string(int status);
 void tss_destroy(tss_ctx* ctx);

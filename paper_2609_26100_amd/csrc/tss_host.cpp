@@ -337,7 +337,8 @@ struct tss_ctx {
 
 namespace {
 
-// message of the last failed tss_create on this thread (tss_last_error(NULL))
+// message of the last failed tss_create or operator call on this thread
+// (tss_last_error(NULL))
 std::string& create_error() {
   static thread_local std::string e = "null context";
   return e;
@@ -1798,8 +1799,15 @@ int tss_get_greedy(tss_ctx* c, int32_t* host_dst, int32_t n_nodes) {
 }  // extern "C"
 
 // Internal interface of tss_verify_static (tss_static.hip, which holds the
-// static scratch).
+// static scratch) and of the operators (tss_ops.cpp).
 namespace tss {
+
+void set_thread_error(const char* msg) {
+  try {
+    create_error() = msg;
+  } catch (...) {  // no memory for the message
+  }
+}
 
 int static_prepare(tss_ctx* c, int32_t seq, int* device) {
   const int r = check_ready(c, seq);

@@ -421,6 +421,50 @@ hipError_t launch_prompt_attn(int head_dim, const PromptAttnArgs& a, hipStream_t
 hipError_t init_prompt_attributes();
 hipError_t launch_rope_table(float2* tab, int max_pos, int head_dim, float base, hipStream_t s);
 
+// The operators on the caller's tensors (tss_ops.cpp checks their arguments).
+struct LogprobArgs {
+  const void* x;           // [rows][vocab], rows `stride` elements apart
+  int64_t stride;
+  int rows, vocab, type;   // type: enum tss_tensor_type
+  const int32_t* tokens;   // [rows][n_tokens]
+  int n_tokens, top_k;
+  float* logprob;          // outputs, null where not wanted
+  int32_t* rank;
+  float* entropy;
+  float* top_logprob;
+  int32_t* top_token;
+};
+hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s);
+
+struct WindowArgs {
+  const void* q;           // [rows][n_q_heads][hd], rows q_stride elements apart
+  void* o;
+  int64_t q_stride, o_stride;
+  const uint8_t* kv_pages; // the layer's pages
+  const int32_t* page_table;
+  const int32_t* row_offsets;
+  const int32_t* lengths;
+  int n_pages, n_heads, group;  // kv heads, query heads of each
+  int n_seqs, table_stride, rows;
+  int max_rows, max_length;
+  int sinks, window;
+  float scale_log2;        // log2(e) * scale
+};
+hipError_t launch_window(bool f16, int head_dim, const WindowArgs& a, hipStream_t s);
+
+constexpr int kCopyPairs = 448;  // page copies of one launch (by value)
+struct CopyArgs {
+  uint8_t* pages;
+  size_t page_bytes, layer_bytes;
+  int n_layers, n;
+  int32_t src[kCopyPairs], dst[kCopyPairs];
+};
+hipError_t launch_copy_pages(const CopyArgs& a, hipStream_t s);
+
+// Message of the calling thread's last failure outside a context
+// (tss_last_error(NULL)).
+void set_thread_error(const char* msg);
+
 // Host runtime pieces of tss_verify_static (tss_static.hip holds the static
 // scratch): the checks before any device work (sequence state, the model's
 // single-sequence workspace against the scratch size; the context's device),

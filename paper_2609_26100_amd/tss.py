@@ -29,10 +29,13 @@ EXPORTS = (
     "tss_verify_batch", "tss_verify_sweep", "tss_sweep_prefix_bytes", "tss_get_greedy", "tss_get_path", "tss_seq_length", "tss_seq_truncate", "tss_validate_tree", "tss_validate_mask",
     "tss_tree_meta", "tss_set_launch_mode", "tss_profile_kernel", "tss_profile_read", "tss_last_error", "tss_status_string",
     "tss_destroy", "tss_get_logits_device", "tss_get_attn_split", "tss_check_kv", "tss_verify_static",
-    "tss_static_workspace_bytes", "tss_bf16_to_f16",
+    "tss_static_workspace_bytes", "tss_bf16_to_f16", "tss_token_logprobs", "tss_token_logprobs_bytes",
+    "tss_window_attn", "tss_window_attn_bytes", "tss_copy_pages",
 )
 
 TSS_STATIC_SCRATCH_BYTES = 64 << 20
+TSS_T_F32, TSS_T_BF16, TSS_T_F16 = 0, 1, 2
+TSS_LOGPROBS_MAX_TOKENS, TSS_LOGPROBS_MAX_TOP = 8, 32
 
 
 class tss_model_cfg(ctypes.Structure):
@@ -41,6 +44,14 @@ class tss_model_cfg(ctypes.Structure):
         ("head_dim", ctypes.c_int32), ("ffn_dim", ctypes.c_int32), ("vocab", ctypes.c_int32),
         ("rope_base", ctypes.c_float), ("rms_eps", ctypes.c_float), ("dtype", ctypes.c_int32),
         ("max_nodes", ctypes.c_int32), ("max_batch", ctypes.c_int32),
+    ]
+
+
+class tss_paged_kv(ctypes.Structure):
+    _fields_ = [
+        ("pages", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("n_layers", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("type", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("table_stride", ctypes.c_int32),
     ]
 
 
@@ -61,7 +72,7 @@ def lib():
             raise RuntimeError(f"{LIB_PATH} is missing: build it with python -m paper_2609_26100_amd.build")
         L = ctypes.CDLL(LIB_PATH)
         P, I32, U32, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_size_t
-        CFG = ctypes.POINTER(tss_model_cfg)
+        CFG, KV = ctypes.POINTER(tss_model_cfg), ctypes.POINTER(tss_paged_kv)
         sig = {
             "tss_cfg_check": (ctypes.c_int, [CFG]),
             "tss_weights_bytes": (SZ, [CFG]),
@@ -85,6 +96,13 @@ def lib():
                                                  ctypes.POINTER(I32)]),
             "tss_static_workspace_bytes": (SZ, [CFG]),
             "tss_bf16_to_f16": (ctypes.c_int64, [P, P, ctypes.c_int64]),
+            "tss_token_logprobs_bytes": (SZ, [I32, I32, I32, I32]),
+            "tss_token_logprobs": (ctypes.c_int, [P, P, I32, ctypes.c_int64, I32, I32, P, I32, I32, P, P, P, P, P, P,
+                                                  SZ]),
+            "tss_window_attn_bytes": (SZ, [KV, I32, I32, I32, I32, I32, I32]),
+            "tss_window_attn": (ctypes.c_int, [P, KV, I32, P, ctypes.c_int64, I32, P, P, I32, I32, I32, I32, I32,
+                                               ctypes.c_float, P, ctypes.c_int64, P, SZ]),
+            "tss_copy_pages": (ctypes.c_int, [P, KV, P, P, I32]),
             "tss_get_path": (ctypes.c_int, [P, I32, P, ctypes.POINTER(I32)]),
             "tss_seq_length": (ctypes.c_int, [P, I32, ctypes.POINTER(I32)]),
             "tss_seq_truncate": (ctypes.c_int, [P, I32, I32]),
@@ -113,6 +131,11 @@ def _ptr(a):
     if not a.flags["C_CONTIGUOUS"]:
         raise ValueError("array must be C-contiguous")
     return a.ctypes.data
+
+
+def _check_op(status):
+    if status != TSS_OK:
+        raise TSSError(status, tss_last_error(None))
 
 
 def _check(status, ctx=None, what=""):
@@ -332,6 +355,38 @@ def tss_profile_read(ctx, reset=False):
     ms, n = ctypes.c_double(), ctypes.c_int64()
     _check(lib().tss_profile_read(ctx, ctypes.byref(ms), ctypes.byref(n), int(reset)), ctx, "tss_profile_read")
     return ms.value, n.value
+
+
+def tss_token_logprobs_bytes(rows, vocab, n_tokens, top_k) -> int:
+    return lib().tss_token_logprobs_bytes(rows, vocab, n_tokens, top_k)
+
+
+def tss_token_logprobs(hip_stream, logits, type, row_stride, rows, vocab, tokens, n_tokens, top_k, logprob, rank,
+                       entropy, top_logprob, top_token, workspace, workspace_bytes):
+    """Every tensor is a device address (or None)."""
+    _check_op(lib().tss_token_logprobs(hip_stream, logits, type, row_stride, rows, vocab, tokens, n_tokens, top_k,
+                                       logprob, rank, entropy, top_logprob, top_token, workspace, workspace_bytes))
+
+
+def tss_window_attn_bytes(kv, n_q_heads, rows, max_rows, max_length, sinks, window) -> int:
+    return lib().tss_window_attn_bytes(kv, n_q_heads, rows, max_rows, max_length, sinks, window)
+
+
+def tss_window_attn(hip_stream, kv, layer, q, q_stride, n_q_heads, row_offsets, lengths, rows, max_rows, max_length,
+                    sinks, window, scale, out, out_stride, workspace, workspace_bytes):
+    """kv: a tss_paged_kv; every tensor is a device address (or None)."""
+    _check_op(lib().tss_window_attn(hip_stream, kv, layer, q, q_stride, n_q_heads, row_offsets, lengths, rows,
+                                    max_rows, max_length, sinks, window, scale, out, out_stride, workspace,
+                                    workspace_bytes))
+
+
+def tss_copy_pages(hip_stream, kv, src, dst):
+    """kv: a tss_paged_kv; src and dst: host lists of page ids."""
+    s = np.ascontiguousarray(src, dtype=np.int32)
+    d = np.ascontiguousarray(dst, dtype=np.int32)
+    if s.ndim != 1 or s.shape != d.shape:
+        raise ValueError("src and dst must be lists of one length")
+    _check_op(lib().tss_copy_pages(hip_stream, kv, _ptr(s), _ptr(d), len(s)))
 
 
 def tss_last_error(ctx) -> str:

@@ -1,0 +1,142 @@
+"""What the operators refuse, on the CPU: every check comes before any device work, so the addresses need not exist."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2609_26100_amd import ops
+from paper_2609_26100_amd import tss as abi
+
+P = 0x10000  # a device address that no check touches
+
+
+def logprobs(**kw):
+    a = dict(logits=P, type=abi.TSS_T_F32, row_stride=100, rows=2, vocab=100, tokens=P, n_tokens=1, top_k=5, logprob=P,
+             rank=P, entropy=P, top_logprob=P, top_token=P, workspace=P, workspace_bytes=1 << 30)
+    a.update(kw)
+    abi.tss_token_logprobs(None, **a)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(type=3), dict(type=-1), dict(rows=-1), dict(vocab=0), dict(row_stride=99), dict(n_tokens=9),
+    dict(n_tokens=-1), dict(top_k=33), dict(top_k=-1), dict(vocab=4, top_k=5), dict(logits=None), dict(tokens=None),
+    dict(logits=P + 2), dict(type=abi.TSS_T_F16, logits=P + 1)])
+def test_logprobs_refuses(bad):
+    with pytest.raises(abi.TSSError) as e:
+        logprobs(**bad)
+    assert e.value.status == abi.TSS_EINVAL and "tss_token_logprobs" in str(e.value)
+
+
+def test_logprobs_workspace():
+    need = abi.tss_token_logprobs_bytes(1, 1 << 20, 1, 32)
+    if need:
+        for bad in (dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=P + 8)):
+            with pytest.raises(abi.TSSError) as e:
+                logprobs(**dict(dict(rows=1, vocab=1 << 20, row_stride=1 << 20, top_k=32), **bad))
+            assert e.value.status == abi.TSS_ENOSPACE
+    logprobs(rows=0)                       # nothing to do
+    logprobs(rows=0, logits=None, tokens=None)
+    for bad in ((-1, 100, 1, 1), (1, 0, 1, 1), (1, 100, 9, 1), (1, 100, 1, 33), (1, 4, 0, 5)):
+        assert abi.tss_token_logprobs_bytes(*bad) == 0
+
+
+def cache(**kw):
+    kv = abi.tss_paged_kv(P, P, 2, 8, 4, 64, abi.TSS_T_F16, 2, 4)
+    for k, v in kw.items():
+        setattr(kv, k, v)
+    return kv
+
+
+def window(kv=None, **kw):
+    a = dict(layer=0, q=P, q_stride=512, n_q_heads=8, row_offsets=P, lengths=P, rows=4, max_rows=4, max_length=64,
+             sinks=1, window=16, scale=0.0, out=P, out_stride=512, workspace=P, workspace_bytes=1 << 40)
+    a.update(kw)
+    abi.tss_window_attn(None, kv or cache(), **a)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(layer=2), dict(layer=-1), dict(q_stride=511), dict(q_stride=504), dict(q_stride=516), dict(out_stride=8),
+    dict(n_q_heads=6), dict(n_q_heads=0), dict(rows=-1), dict(max_rows=-1), dict(max_length=-1), dict(sinks=-1),
+    dict(window=-1), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(q=None),
+    dict(out=None), dict(row_offsets=None), dict(lengths=None), dict(q=P + 8), dict(out=P + 4)])
+def test_window_refuses(bad):
+    with pytest.raises(abi.TSSError) as e:
+        window(**bad)
+    assert e.value.status == abi.TSS_EINVAL and "tss_window_attn" in str(e.value)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(pages=None), dict(type=abi.TSS_T_BF16), dict(type=7), dict(head_dim=96), dict(n_layers=0), dict(n_pages=0),
+    dict(n_kv_heads=0), dict(n_kv_heads=65536), dict(pages=P + 8)])
+def test_cache_refused(bad):
+    for call in (window, lambda kv: abi.tss_copy_pages(None, kv, [0], [1])):
+        with pytest.raises(abi.TSSError) as e:
+            call(cache(**bad))
+        assert e.value.status == abi.TSS_EINVAL
+
+
+def test_window_table_and_workspace():
+    for bad in (dict(page_table=None), dict(n_seqs=-1), dict(table_stride=0)):
+        with pytest.raises(abi.TSSError):
+            window(cache(**bad))
+    kv = cache(n_pages=1 << 16, table_stride=1 << 14, n_seqs=1)
+    big = dict(rows=1, max_rows=1, max_length=1 << 18, window=0)
+    need = abi.tss_window_attn_bytes(kv, 8, 1, 1, 1 << 18, 1, 0)
+    if need:
+        for bad in (dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=P + 8)):
+            with pytest.raises(abi.TSSError) as e:
+                window(kv, **big, **bad)
+            assert e.value.status == abi.TSS_ENOSPACE
+    for nothing in (dict(rows=0), dict(max_rows=0)):
+        window(**nothing, q=None, out=None)
+    window(cache(n_seqs=0), row_offsets=None, lengths=None)
+    assert abi.tss_window_attn_bytes(cache(head_dim=96), 8, 4, 4, 64, 1, 16) == 0
+    assert abi.tss_window_attn_bytes(cache(), 7, 4, 4, 64, 1, 16) == 0
+
+
+@pytest.mark.parametrize("src,dst", [([0], [8]), ([8], [0]), ([-1], [0]), ([0], [-1]), ([0, 1], [2, 2]), ([0], [0]),
+                                     ([0, 1], [1, 2]), ([0, 2], [1, 0])])
+def test_copy_refuses(src, dst):
+    with pytest.raises(abi.TSSError) as e:
+        abi.tss_copy_pages(None, cache(), src, dst)
+    assert e.value.status == abi.TSS_EINVAL
+
+
+def test_copy_lists():
+    abi.tss_copy_pages(None, cache(), [], [])
+    with pytest.raises(ValueError):
+        abi.tss_copy_pages(None, cache(), [0, 1], [2])
+    L = abi.lib()
+    assert L.tss_copy_pages(None, ctypes.byref(cache()), None, None, 1) == abi.TSS_EINVAL
+    assert L.tss_copy_pages(None, ctypes.byref(cache()), P, P, -1) == abi.TSS_EINVAL
+    assert L.tss_copy_pages(None, None, P, P, 0) == abi.TSS_EINVAL
+
+
+def test_tensors_off_the_gpu_are_refused():
+    x = torch.zeros(2, 10)
+    pages = torch.zeros(1, 2, 2, 1, 16 * 64)
+    with pytest.raises(ValueError):
+        ops.token_logprobs(x)
+    with pytest.raises(ValueError):
+        ops.copy_pages(pages, [0], [1])
+    with pytest.raises(ValueError):
+        ops.window_attention(torch.zeros(1, 1, 64), pages, None, None, None)
+
+
+@pytest.mark.parametrize("n,heads,hd", [(1, 1, 64), (16, 2, 128), (37, 3, 64)])
+def test_pages_and_back(n, heads, hd):
+    g = torch.Generator().manual_seed(n)
+    k, v = (torch.randn(n, heads, hd, generator=g).half() for _ in range(2))
+    p = ops.pack_pages(k, v)
+    assert p.shape == (-(-n // 16), 2, heads, 16 * hd)
+    t, d = n - 1, hd - 3  # one element where the layout puts it
+    assert p[t // 16, 0, heads - 1].reshape(16, hd)[t % 16, d] == k[t, heads - 1, d]
+    assert p[t // 16, 1, heads - 1].reshape(4, hd, 4)[t % 16 // 4, d, t % 4] == v[t, heads - 1, d]
+    k2, v2 = ops.unpack_pages(p)
+    assert torch.equal(k2[:n], k) and torch.equal(v2[:n], v) and not k2[n:].any() and not v2[n:].any()
+
+
+def test_message_names_the_last_refusal():
+    with pytest.raises(abi.TSSError) as e:
+        logprobs(top_k=40)
+    assert abi.tss_last_error(None) in str(e.value) and "top_k" in abi.tss_last_error(None)
