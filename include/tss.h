@@ -422,7 +422,9 @@ enum tss_tensor_type { TSS_T_F32 = 0, TSS_T_BF16 = 1, TSS_T_F16 = 2 };
  * +inf gets NaN logprobs and entropy, its ranks and alternatives as ordered.
  *   workspace: tss_token_logprobs_bytes() bytes of device memory, aligned to
  *     16 (0 bytes: may be NULL); contents are of no meaning before and after.
- * rows = 0 is allowed and launches nothing.  Paper: Algorithm 1 (the downstream
+ * rows = 0 is allowed and launches nothing; vocab goes up to 2^20, and rows times
+ * the 8192-token chunks of the vocabulary (1 up to 32761 tokens) up to 2^22.
+ * Paper: Algorithm 1 (the downstream
  * metric of a task whose answer is the most probable of several). */
 size_t tss_token_logprobs_bytes(int32_t rows, int32_t vocab, int32_t n_tokens, int32_t top_k);
 int tss_token_logprobs(void* hip_stream, const void* logits, int32_t type, int64_t row_stride, int32_t rows,

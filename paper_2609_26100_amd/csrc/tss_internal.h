@@ -434,7 +434,11 @@ struct LogprobArgs {
   float* top_logprob;
   int32_t* top_token;
 };
-hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s);
+// Limits of a call: logprobs_fit is whether its workgroups can be launched.
+constexpr int kLogprobVocab = 1 << 20;
+bool logprobs_fit(int rows, int vocab);
+size_t logprobs_bytes(int rows, int vocab, int n_tokens, int top_k);
+hipError_t launch_logprobs(const LogprobArgs& a, void* workspace, hipStream_t s);
 
 struct WindowArgs {
   const void* q;           // [rows][n_q_heads][hd], rows q_stride elements apart
@@ -452,7 +456,7 @@ struct WindowArgs {
 };
 hipError_t launch_window(bool f16, int head_dim, const WindowArgs& a, hipStream_t s);
 
-constexpr int kCopyPairs = 448;  // page copies of one launch (by value)
+constexpr int kCopyPairs = 480;  // page copies of one launch (by value)
 struct CopyArgs {
   uint8_t* pages;
   size_t page_bytes, layer_bytes;

@@ -3,6 +3,7 @@
 #include "../../include/tss.h"
 #include "tss_internal.h"
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <vector>
@@ -26,6 +27,15 @@ int type_size(int32_t t) { return t == TSS_T_F32 ? 4 : (t == TSS_T_BF16 || t == 
 
 bool aligned(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 
+// What is wrong with the sizes of a call, or null.
+const char* logprobs_fault(int32_t rows, int32_t vocab, int32_t n_tokens, int32_t top_k) {
+  if (rows < 0 || vocab < 1) return "bad rows or vocab";
+  if (n_tokens < 0 || n_tokens > TSS_LOGPROBS_MAX_TOKENS || top_k < 0 || top_k > TSS_LOGPROBS_MAX_TOP || top_k > vocab)
+    return "n_tokens outside [0, 8] or top_k outside [0, min(32, vocab)]";
+  if (!logprobs_fit(rows, vocab)) return "more than 2^20 tokens in the vocabulary, or too many rows for one launch";
+  return nullptr;
+}
+
 // What is wrong with a cache's description, or null.
 const char* kv_fault(const tss_paged_kv* kv) {
   if (!kv || !kv->pages) return "no cache";
@@ -33,6 +43,7 @@ const char* kv_fault(const tss_paged_kv* kv) {
   if (kv->head_dim != 64 && kv->head_dim != 128) return "head_dim must be 64 or 128";
   if (kv->n_layers < 1 || kv->n_pages < 1 || kv->n_kv_heads < 1 || kv->n_kv_heads > 65535)
     return "layers, pages and heads must be positive (heads up to 65535)";
+  if (kv->n_layers > kMaxLayers) return "too many layers";
   if (!aligned(kv->pages, 16)) return "pages must be aligned to 16 bytes";
   return nullptr;
 }
@@ -45,7 +56,9 @@ size_t page_bytes(const tss_paged_kv* kv) {
 
 extern "C" {
 
-size_t tss_token_logprobs_bytes(int32_t, int32_t, int32_t, int32_t) { return 0; }
+size_t tss_token_logprobs_bytes(int32_t rows, int32_t vocab, int32_t n_tokens, int32_t top_k) {
+  return logprobs_fault(rows, vocab, n_tokens, top_k) ? 0 : logprobs_bytes(rows, vocab, n_tokens, top_k);
+}
 
 int tss_token_logprobs(void* hip_stream, const void* logits, int32_t type, int64_t row_stride, int32_t rows,
                        int32_t vocab, const int32_t* tokens, int32_t n_tokens, int32_t top_k, float* logprob,
@@ -54,13 +67,12 @@ int tss_token_logprobs(void* hip_stream, const void* logits, int32_t type, int64
   const char* me = "tss_token_logprobs";
   const int es = type_size(type);
   if (!es) return refuse(TSS_EINVAL, me, "unknown element type");
-  if (rows < 0 || vocab < 1 || row_stride < vocab) return refuse(TSS_EINVAL, me, "bad rows, vocab or row_stride");
-  if (n_tokens < 0 || n_tokens > TSS_LOGPROBS_MAX_TOKENS || top_k < 0 || top_k > TSS_LOGPROBS_MAX_TOP || top_k > vocab)
-    return refuse(TSS_EINVAL, me, "n_tokens outside [0, 8] or top_k outside [0, min(32, vocab)]");
+  if (const char* f = logprobs_fault(rows, vocab, n_tokens, top_k)) return refuse(TSS_EINVAL, me, f);
+  if (row_stride < vocab) return refuse(TSS_EINVAL, me, "row_stride smaller than vocab");
   if (rows == 0) return TSS_OK;
   if (!logits || (n_tokens > 0 && !tokens)) return refuse(TSS_EINVAL, me, "null tensor");
   if (!aligned(logits, es)) return refuse(TSS_EINVAL, me, "logits must be aligned to their elements");
-  const size_t need = tss_token_logprobs_bytes(rows, vocab, n_tokens, top_k);
+  const size_t need = logprobs_bytes(rows, vocab, n_tokens, top_k);
   if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16)))
     return refuse(TSS_ENOSPACE, me, "workspace smaller than tss_token_logprobs_bytes() or not aligned to 16 bytes");
   LogprobArgs a{};
@@ -77,7 +89,7 @@ int tss_token_logprobs(void* hip_stream, const void* logits, int32_t type, int64
   a.entropy = entropy;
   a.top_logprob = top_logprob;
   a.top_token = top_token;
-  return launched(launch_logprobs(a, (hipStream_t)hip_stream), me);
+  return launched(launch_logprobs(a, workspace, (hipStream_t)hip_stream), me);
 }
 
 size_t tss_window_attn_bytes(const tss_paged_kv*, int32_t, int32_t, int32_t, int32_t, int32_t, int32_t) { return 0; }
@@ -130,6 +142,11 @@ int tss_copy_pages(void* hip_stream, const tss_paged_kv* kv, const int32_t* src,
   const char* me = "tss_copy_pages";
   if (const char* f = kv_fault(kv)) return refuse(TSS_EINVAL, me, f);
   if (n < 0 || (n > 0 && (!src || !dst))) return refuse(TSS_EINVAL, me, "bad list of pages");
+  CopyArgs a{};
+  a.pages = (uint8_t*)kv->pages;
+  a.page_bytes = page_bytes(kv);
+  a.layer_bytes = a.page_bytes * kv->n_pages;
+  a.n_layers = kv->n_layers;
   try {
     std::vector<uint8_t> use(kv->n_pages, 0);  // 1: a source, 2: a destination
     for (int i = 0; i < n; ++i) {
@@ -141,21 +158,20 @@ int tss_copy_pages(void* hip_stream, const tss_paged_kv* kv, const int32_t* src,
     }
     for (int i = 0; i < n; ++i)
       if (use[src[i]] == 3) return refuse(TSS_EINVAL, me, "a page is source and destination");
-  } catch (...) {
-    return refuse(TSS_ENOSPACE, me, "no host memory to check the list");
-  }
-  CopyArgs a{};
-  a.pages = (uint8_t*)kv->pages;
-  a.page_bytes = page_bytes(kv);
-  a.layer_bytes = a.page_bytes * kv->n_pages;
-  a.n_layers = kv->n_layers;
-  for (int i0 = 0; i0 < n; i0 += kCopyPairs) {
-    a.n = n - i0 < kCopyPairs ? n - i0 : kCopyPairs;
-    for (int i = 0; i < a.n; ++i) {
-      a.src[i] = src[i0 + i];
-      a.dst[i] = dst[i0 + i];
+    // copies of one source next to each other: it is read once for them
+    std::vector<int32_t> order(n);
+    for (int i = 0; i < n; ++i) order[i] = i;
+    std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) { return src[x] < src[y]; });
+    for (int i0 = 0; i0 < n; i0 += kCopyPairs) {
+      a.n = std::min(n - i0, kCopyPairs);
+      for (int i = 0; i < a.n; ++i) {
+        a.src[i] = src[order[i0 + i]];
+        a.dst[i] = dst[order[i0 + i]];
+      }
+      if (const int r = launched(launch_copy_pages(a, (hipStream_t)hip_stream), me)) return r;
     }
-    if (const int r = launched(launch_copy_pages(a, (hipStream_t)hip_stream), me)) return r;
+  } catch (...) {
+    return refuse(TSS_ENOSPACE, me, "no host memory for the list");
   }
   return TSS_OK;
 }
