@@ -7,8 +7,7 @@
 // 16-byte loads, so HBM is read once, and goes over the registers twice: for
 // the maxima, and for S, T, the ranks and the candidates of the alternatives.
 //   * Ranks: a token's rank is the number of logits that come before it, one
-//     compare and a scalar popcount each; equal logits (the token's own, mostly)
-//     are looked at again only by the waves that hold some.
+//     compare and one addition each.
 //   * Alternatives: with W waves, every wave finds the ceil(k / W)-th largest of
 //     its lanes' maxima (its top 16 bits, by bisection over ballots).  The least
 //     of these has at least k logits at or above it, and few more: those
@@ -21,6 +20,8 @@
 #include "../../include/tss.h"
 #include "tss_internal.h"
 
+#include <type_traits>
+
 namespace tss {
 
 namespace {
@@ -28,7 +29,7 @@ namespace {
 constexpr int kLpVals = 32;       // logits a thread holds
 constexpr int kLpList = 512;      // candidates in LDS
 constexpr int kLpTokens = TSS_LOGPROBS_MAX_TOKENS;
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 typedef unsigned long long u64;
 
@@ -82,10 +83,46 @@ __device__ __forceinline__ float key_value(unsigned k) {
 // Key of (logit, token): the lower token first among equal logits.  Never 0.
 __device__ __forceinline__ u64 pair_key(float x, int i) { return ((u64)order_key(x) << 32) | (unsigned)~i; }
 
+// The same value, of which the compiler does not know it: what a rare path
+// computes again from it is not kept in registers from the first time.
+__device__ __forceinline__ float again(float x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// All lanes' values joined by f, for every lane (a scalar), in a fixed order, by
+// DPP moves: no trip through LDS.  none: f's neutral value.
 template <typename V, typename F>
-__device__ __forceinline__ V wave_reduce(V v, F f) {
+__device__ __forceinline__ V wave_reduce(V v, V none, F f) {
+  auto move = [&](auto ctrl, auto rows) {
+    const int m = __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v),
+                                              decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+    v = f(v, __builtin_bit_cast(V, m));
+  };
+  using std::integral_constant;
+  move(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});  // from 1, 2, 4, 8 lanes before in the row
+  move(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+  move(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+  move(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+  move(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});  // a row's last lane to the next row
+  move(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});  // lane 31 to the upper half
+  return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  return wave_reduce(v, 0.f, [](float p, float q) { return p + q; });
+}
+__device__ __forceinline__ float wave_max(float v) {
+  return wave_reduce(v, -INFINITY, [](float p, float q) { return fmaxf(p, q); });
+}
+__device__ __forceinline__ int wave_sum(int v) {
+  return wave_reduce(v, 0, [](int p, int q) { return p + q; });
+}
+__device__ __forceinline__ u64 wave_max(u64 v) {
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v = f(v, __shfl_xor(v, off));
+  for (int off = 32; off >= 1; off >>= 1) {
+    const u64 o = __shfl_xor(v, off);
+    v = o > v ? o : v;
+  }
   return v;
 }
 
@@ -125,7 +162,8 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
   __shared__ float s_m[W], s_S[W], s_T[W];
   __shared__ unsigned s_key[W];
   __shared__ int s_count[W][kLpTokens];
-  __shared__ u64 s_list[kLpList], s_best[W];
+  __shared__ __align__(16) u64 s_list[kLpList];
+  __shared__ u64 s_best[W];
   __shared__ int s_n;
   const int r = PARTS ? blockIdx.x / chunks : blockIdx.x, chunk = PARTS ? blockIdx.x % chunks : 0;
   const int V = a.vocab, tid = threadIdx.x, lane = tid & 63;
@@ -148,21 +186,30 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
       for (int e = 0; e < VE; ++e) x[v * VE + e] = t0 + e >= 0 && t0 + e < V ? L::at(row, t0 + e) : -INFINITY;
     }
   }
-  float xt[kLpTokens];
-  int tok[kLpTokens];
-#pragma unroll
-  for (int t = 0; t < kLpTokens; ++t)
-    if (t < a.n_tokens) {
-      tok[t] = a.tokens[(size_t)r * a.n_tokens + t];
-      xt[t] = tok[t] >= 0 && tok[t] < V ? L::at(row, tok[t]) : 0.f;
+  // what the rare paths read: the thread's logits from the cache again, so that
+  // they take no registers from the common ones
+  auto each = [&](auto f) {
+#pragma unroll 8
+    for (int i = 0; i < kLpVals; ++i) {
+      const int k = token(i);
+      if (k >= 0 && k < V) f(L::at(row, k), k);
     }
+  };
+  // lane t of every wave has given token t and its logit
+  int tok = -1;
+  float xt = 0.f;
+  if (lane < a.n_tokens) {
+    tok = a.tokens[(size_t)r * a.n_tokens + lane];
+    if (tok >= 0 && tok < V) xt = L::at(row, tok);
+  }
+  for (int i = tid; i < kLpList; i += TH) s_list[i] = 0;
   if (tid == 0) s_n = 0;
 
   float lm = x[0];
 #pragma unroll
   for (int i = 1; i < kLpVals; ++i) lm = fmaxf(lm, x[i]);
   lm = lm != lm ? -INFINITY : lm;
-  const float wm = wave_reduce(lm, [](float p, float q) { return fmaxf(p, q); });
+  const float wm = wave_max(lm);
   unsigned cut = 0;
   if (a.top_k > 0) {
     const unsigned k = order_key(lm);
@@ -188,56 +235,92 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
   }
   const float base = rs.base();
 
+  // (x - m) log2 e as one fma: the rounding of m log2 e shifts all of them by
+  // the same `shift`, which is taken out of the sums again
+  const float b2 = base * kLog2e, shift = fmaf(base, kLog2e, -b2);
   float S = 0.f, T = 0.f;
 #pragma unroll
   for (int i = 0; i < kLpVals; ++i) {
-    const float d = x[i] - base, e = __builtin_amdgcn_exp2f(d * kLog2e);
+    const float d = fmaf(x[i], kLog2e, -b2), e = __builtin_amdgcn_exp2f(d);
     S += e;
-    T += e * fmaxf(d, -1e30f);  // d = -inf has e = 0
+    T = fmaf(e, d, T);
   }
-  S = wave_reduce(S, [](float p, float q) { return p + q; });
-  T = wave_reduce(T, [](float p, float q) { return p + q; });
+  if (fabsf(base) > 1e30f) {  // m log2 e may overflow
+    S = T = 0.f;
+    const float base2 = again(base);
 #pragma unroll
-  for (int t = 0; t < kLpTokens; ++t)
-    if (t < a.n_tokens) {
-      int n = 0;
-      const float y = xt[t];
-      u64 equal = 0;
-      if (y == y) {
-#pragma unroll
-        for (int i = 0; i < kLpVals; ++i) {
-          n += __popcll(__ballot(!(x[i] <= y)));
-          equal |= __ballot(x[i] == y);
-        }
-      } else {
-        equal = ~0ull;
-      }
-      if (equal) {
-#pragma unroll
-        for (int i = 0; i < kLpVals; ++i) {
-          const int k = token(i);
-          n += __popcll(__ballot((x[i] == y || (x[i] != x[i] && y != y)) && k >= 0 && k < tok[t]));
-        }
-      }
-      if (lane == 0) s_count[wave][t] = n;
+    for (int i = 0; i < kLpVals; ++i) {
+      const float d = x[i] - base2, e = __builtin_amdgcn_exp2f(d * kLog2e);
+      S += e;
+      T = e == 0.f ? T : fmaf(e, d, T);
     }
+  } else {
+    if (__any(T != T)) {  // logits of -inf have e = 0 (where it is not NaN for good)
+      T = 0.f;
+      const float b3 = again(b2);
+#pragma unroll
+      for (int i = 0; i < kLpVals; ++i) {
+        const float d = fmaf(x[i], kLog2e, -b3), e = __builtin_amdgcn_exp2f(d);
+        T = e == 0.f ? T : fmaf(e, d, T);
+      }
+    }
+    const float f = __builtin_amdgcn_exp2f(-shift);
+    T = (T - shift * S) * f * kLn2;
+    S *= f;
+  }
+  S = wave_sum(S);
+  T = wave_sum(T);
+  for (int t = 0; t < a.n_tokens; ++t) {
+    int n = 0;
+    const float y = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(xt), t));
+    const int at = __builtin_amdgcn_readlane(tok, t);
+    if (fabsf(y) < INFINITY) {
+      // before the token an equal logit counts, behind it only a larger one:
+      // at least y, or at least the float after it; a block that holds the
+      // token counts as behind
+      const float up = y == 0.f ? __uint_as_float(1u) : __uint_as_float(__float_as_uint(y) + (y > 0.f ? 1u : -1u));
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int t0 = token(v * VE);
+        const float c = t0 + VE <= at ? y : up;
+#pragma unroll
+        for (int e = 0; e < VE; ++e) n += !(x[v * VE + e] < c);
+        if (t0 <= at && at < t0 + VE) {
+#pragma unroll
+          for (int e = 0; e < VE; ++e) n += x[v * VE + e] == y && t0 + e < at;
+        }
+      }
+    } else {
+      each([&](float z, int k) { n += pair_key(z, k) > pair_key(y, at); });
+    }
+    n = wave_sum(n);
+    if (lane == 0) s_count[wave][t] = n;
+  }
   if (lane == 0) {
     s_S[wave] = S;
     s_T[wave] = T;
   }
   if (a.top_k > 0) {
-    // everything at or above the cut; where the cut is at -inf, of the logits
-    // of -inf only the chunk's first top_k tokens
-    const float c = cut > order_key(-INFINITY) ? key_value(cut) : -INFINITY;
+    // everything at or above the cut, a bit for each; where the cut is at
+    // -inf, of the logits of -inf only the chunk's first top_k tokens
+    const bool all = cut <= order_key(-INFINITY);
+    const float c = all ? -INFINITY : key_value(cut);
     const int early = max(0, chunk * (TH * NV) * VE - skew) + a.top_k;
+    unsigned take = 0;
 #pragma unroll
-    for (int i = 0; i < kLpVals; ++i) {
-      if (!(x[i] < c)) {
+    for (int i = kLpVals - 1; i >= 0; --i) take = 2 * take + !(x[i] < c);
+    if (all) {
+#pragma unroll
+      for (int i = 0; i < kLpVals; ++i) {
         const int k = token(i);
-        if (x[i] != -INFINITY || (k >= 0 && k < V && k < early)) {
-          const int at = atomicAdd(&s_n, 1);
-          if (at < kLpList) s_list[at] = pair_key(x[i], k);
-        }
+        if (x[i] == -INFINITY && (k < 0 || k >= V || k >= early)) take &= ~(1u << i);
+      }
+    }
+    if (take) {  // a few lanes have one; its logit once more, by its token
+      int at = atomicAdd(&s_n, __popc(take));
+      for (; take && at < kLpList; take &= take - 1, ++at) {
+        const int k = token(__builtin_ctz(take));
+        s_list[at] = pair_key(L::at(row, k), k);
       }
     }
   }
@@ -256,9 +339,7 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
     if constexpr (PARTS) {
       parts.counts[part * a.n_tokens + tid] = n;
     } else {
-      const size_t at = (size_t)r * a.n_tokens + tid;
-      const int k = a.tokens[at];
-      write_token(a, at, rs, k, k >= 0 && k < V ? L::at(row, k) : 0.f, n);
+      write_token(a, (size_t)r * a.n_tokens + tid, rs, tok, xt, n);
     }
   }
   if (tid == 0) {
@@ -282,7 +363,10 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
     for (int i = tid; i < n; i += TH) {
       const u64 k = s_list[i];
       int place = 0;
-      for (int j = 0; j < n; ++j) place += s_list[j] > k;
+      for (int j = 0; j < n; j += 8) {  // zeros behind the last
+#pragma unroll
+        for (int u = 0; u < 8; ++u) place += s_list[j + u] > k;
+      }
       if (place < a.top_k) put(place, k);
     }
     for (int i = n + tid; i < a.top_k; i += TH) put(i, 0);
@@ -294,14 +378,12 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
   for (int t = 0; t < a.top_k; ++t) {
     if (stale) {
       mine = 0;
-#pragma unroll
-      for (int i = 0; i < kLpVals; ++i) {
-        const int tk = token(i);
-        const u64 k = tk >= 0 && tk < V ? pair_key(x[i], tk) : 0;
+      each([&](float z, int token) {
+        const u64 k = pair_key(z, token);
         if (k < taken && k > mine) mine = k;
-      }
+      });
     }
-    const u64 best = wave_reduce(mine, [](u64 p, u64 q) { return p > q ? p : q; });
+    const u64 best = wave_max(mine);
     __syncthreads();
     if (lane == 0) s_best[wave] = best;
     __syncthreads();
