@@ -6,15 +6,17 @@
 // A workgroup takes a chunk of a row, 32 logits a thread, into registers with
 // 16-byte loads, so HBM is read once, and goes over the registers twice: for
 // the maxima, and for S, T, the ranks and the candidates of the alternatives.
-//   * Ranks: a token's rank is the number of logits that come before it, one
-//     compare and one addition each.
+//   * Ranks: a token's rank is the number of logits that come before it: the sign
+//     of a difference each (a compare's mask in a scalar register would make the
+//     next instruction wait).
 //   * Alternatives: with W waves, every wave finds the ceil(k / W)-th largest of
 //     its lanes' maxima (its top 16 bits, by bisection over ballots).  The least
-//     of these has at least k logits at or above it, and few more: those
-//     go to LDS, where each counts how many precede it.  Keys of (logit,
-//     token) are unique, so the order in which they got there does not matter.
-//     Where too many are equal for the LDS list, the k first are taken out one
-//     by one instead.
+//     of these has at least k logits at or above it, and few more.  Only
+//     threads whose maximum reaches it hold any: they are listed, all threads
+//     look through theirs, and what is found goes to a list in LDS, where each
+//     counts how many precede it.  Keys of (logit, token) are unique, so the
+//     order in which they got there does not matter.  Where too many are equal
+//     for the list, the k first are taken out one by one instead.
 // Rows of more than one chunk leave (m, S, T), counts and k keys for each chunk in the
 // workspace and a second launch joins them.
 #include "../../include/tss.h"
@@ -117,6 +119,10 @@ __device__ __forceinline__ float wave_max(float v) {
 __device__ __forceinline__ int wave_sum(int v) {
   return wave_reduce(v, 0, [](int p, int q) { return p + q; });
 }
+// bits shifted up by one, the sign of d below them.
+__device__ __forceinline__ unsigned push_sign(unsigned bits, float d) {
+  return __builtin_amdgcn_alignbit(bits, __float_as_uint(d), 31);
+}
 __device__ __forceinline__ u64 wave_max(u64 v) {
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) {
@@ -154,9 +160,9 @@ __device__ __forceinline__ void write_top(const LogprobArgs& a, size_t at, const
   if (a.top_token) a.top_token[at] = (int)~(unsigned)key;
 }
 
-// One workgroup per row and chunk.  PARTS: the chunk's share goes to the workspace.
+// grid (rows, chunks).  PARTS: the chunk's share goes to the workspace.
 template <int TYPE, int W, bool PARTS>
-__global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts, int chunks) {
+__global__ __launch_bounds__(W * 64, PARTS ? 6 : 1) void k_logprobs(LogprobArgs a, Parts parts, int chunks) {
   using L = Logit<TYPE>;
   constexpr int VE = 16 / L::size, NV = kLpVals / VE, TH = W * 64;
   __shared__ float s_m[W], s_S[W], s_T[W];
@@ -164,8 +170,8 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
   __shared__ int s_count[W][kLpTokens];
   __shared__ __align__(16) u64 s_list[kLpList];
   __shared__ u64 s_best[W];
-  __shared__ int s_n;
-  const int r = PARTS ? blockIdx.x / chunks : blockIdx.x, chunk = PARTS ? blockIdx.x % chunks : 0;
+  __shared__ int s_n, s_holders, s_holder[TH];
+  const int r = blockIdx.x, chunk = PARTS ? blockIdx.y : 0;
   const int V = a.vocab, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint8_t* row = (const uint8_t*)a.x + (size_t)r * a.stride * L::size;
@@ -176,14 +182,29 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
   const int b0 = chunk * (TH * NV) + tid;
   float x[kLpVals];
   auto token = [&](int i) { return (b0 + i / VE * TH) * VE + i % VE - skew; };  // token of x[i]
+  const int c0 = chunk * (TH * NV) * VE - skew;  // the chunk's first token
+  uint4 raw[NV];
+  if (c0 >= 0 && c0 + TH * kLpVals <= V) {
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int t0 = token(v * VE);
-    if (t0 >= 0 && t0 + VE <= V) {
-      L::spread(*(const uint4*)(first + (size_t)(b0 + v * TH) * 16), x + v * VE);
-    } else {
+    for (int v = 0; v < NV; ++v) raw[v] = *(const uint4*)(first + (unsigned)(b0 + v * TH) * 16u);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) x[v * VE + e] = t0 + e >= 0 && t0 + e < V ? L::at(row, t0 + e) : -INFINITY;
+    for (int v = 0; v < NV; ++v) L::spread(raw[v], x + v * VE);
+  } else {
+    // the row's first and last chunk: what lies outside is -inf
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int t0 = token(v * VE);
+      raw[v] = uint4{0, 0, 0, 0};
+      if (t0 >= 0 && t0 + VE <= V) raw[v] = *(const uint4*)(first + (unsigned)(b0 + v * TH) * 16u);
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int t0 = token(v * VE);
+      L::spread(raw[v], x + v * VE);
+      if (t0 < 0 || t0 + VE > V) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) x[v * VE + e] = t0 + e >= 0 && t0 + e < V ? L::at(row, t0 + e) : -INFINITY;
+      }
     }
   }
   // what the rare paths read: the thread's logits from the cache again, so that
@@ -203,7 +224,7 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
     if (tok >= 0 && tok < V) xt = L::at(row, tok);
   }
   for (int i = tid; i < kLpList; i += TH) s_list[i] = 0;
-  if (tid == 0) s_n = 0;
+  if (tid == 0) s_n = s_holders = 0;
 
   float lm = x[0];
 #pragma unroll
@@ -233,7 +254,11 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
     rs.m = fmaxf(rs.m, s_m[w]);
     cut = min(cut, s_key[w]);
   }
-  const float base = rs.base();
+  const float base = rs.base(), cut_value = key_value(cut);
+  auto list = [&](float z, int k) {
+    const int at = atomicAdd(&s_n, 1);
+    if (at < kLpList) s_list[at] = pair_key(z, k);
+  };
 
   // (x - m) log2 e as one fma: the rounding of m log2 e shifts all of them by
   // the same `shift`, which is taken out of the sums again
@@ -268,28 +293,37 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
     T = (T - shift * S) * f * kLn2;
     S *= f;
   }
+  const float lane_S = S;
   S = wave_sum(S);
   T = wave_sum(T);
+  // A logit is less than c where the sign of x - c is set (c = 0 taken as -0).
+  // That is not so for NaN and between infinities, which leave a lane's sum NaN.
+  const bool odd = __any(lane_S != lane_S);
   for (int t = 0; t < a.n_tokens; ++t) {
     int n = 0;
     const float y = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(xt), t));
     const int at = __builtin_amdgcn_readlane(tok, t);
-    if (fabsf(y) < INFINITY) {
+    if (wm < y && !odd) {
+      // nothing of this wave's comes before it
+    } else if (fabsf(y) < INFINITY && !odd) {
       // before the token an equal logit counts, behind it only a larger one:
       // at least y, or at least the float after it; a block that holds the
       // token counts as behind
+      const float same = y == 0.f ? -0.f : y;
       const float up = y == 0.f ? __uint_as_float(1u) : __uint_as_float(__float_as_uint(y) + (y > 0.f ? 1u : -1u));
+      unsigned less = 0;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const int t0 = token(v * VE);
-        const float c = t0 + VE <= at ? y : up;
+        const float c = t0 + VE <= at ? same : up;
 #pragma unroll
-        for (int e = 0; e < VE; ++e) n += !(x[v * VE + e] < c);
+        for (int e = 0; e < VE; ++e) less = push_sign(less, x[v * VE + e] - c);
         if (t0 <= at && at < t0 + VE) {
 #pragma unroll
           for (int e = 0; e < VE; ++e) n += x[v * VE + e] == y && t0 + e < at;
         }
       }
+      n += 32 - __popc(less);
     } else {
       each([&](float z, int k) { n += pair_key(z, k) > pair_key(y, at); });
     }
@@ -301,27 +335,16 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
     s_T[wave] = T;
   }
   if (a.top_k > 0) {
-    // everything at or above the cut, a bit for each; where the cut is at
-    // -inf, of the logits of -inf only the chunk's first top_k tokens
-    const bool all = cut <= order_key(-INFINITY);
-    const float c = all ? -INFINITY : key_value(cut);
-    const int early = max(0, chunk * (TH * NV) * VE - skew) + a.top_k;
-    unsigned take = 0;
-#pragma unroll
-    for (int i = kLpVals - 1; i >= 0; --i) take = 2 * take + !(x[i] < c);
-    if (all) {
-#pragma unroll
-      for (int i = 0; i < kLpVals; ++i) {
-        const int k = token(i);
-        if (x[i] == -INFINITY && (k < 0 || k >= V || k >= early)) take &= ~(1u << i);
-      }
-    }
-    if (take) {  // a few lanes have one; its logit once more, by its token
-      int at = atomicAdd(&s_n, __popc(take));
-      for (; take && at < kLpList; take &= take - 1, ++at) {
-        const int k = token(__builtin_ctz(take));
-        s_list[at] = pair_key(L::at(row, k), k);
-      }
+    // what is at or above the cut: first the threads that hold such a logit,
+    // few, whose logits all threads then share out.  Where the cut is at -inf,
+    // of the logits of -inf only the chunk's first top_k tokens
+    if (cut > order_key(-INFINITY) && !odd) {
+      if (!(lm < cut_value)) s_holder[atomicAdd(&s_holders, 1)] = tid;
+    } else {
+      const int early = max(0, c0) + a.top_k;
+      each([&](float z, int k) {
+        if (order_key(z) >= cut && (z != -INFINITY || k < early)) list(z, k);
+      });
     }
   }
   __syncthreads();
@@ -332,7 +355,7 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
     rs.S += s_S[w];
     rs.T += s_T[w];
   }
-  const size_t part = blockIdx.x;
+  const size_t part = (size_t)r * chunks + chunk;
   if (tid < a.n_tokens) {
     int n = 0;
     for (int w = 0; w < W; ++w) n += s_count[w][tid];
@@ -352,6 +375,14 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
     }
   }
   if (a.top_k == 0) return;
+  for (int i = tid; i < s_holders * kLpVals; i += TH) {
+    const int j = i % kLpVals, h = s_holder[i / kLpVals];
+    const int k = (chunk * (TH * NV) + h + j / VE * TH) * VE + j % VE - skew;
+    if (k < 0 || k >= V) continue;
+    const float z = L::at(row, k);
+    if (!(z < cut_value)) list(z, k);
+  }
+  __syncthreads();
   auto put = [&](int place, u64 key) {
     if constexpr (PARTS)
       parts.keys[part * a.top_k + place] = key;
@@ -395,6 +426,12 @@ __global__ __launch_bounds__(W * 64) void k_logprobs(LogprobArgs a, Parts parts,
   }
 }
 
+// sum (x - to) e^(x - to) of terms with sums S and T = sum (x - m) e^(x - m),
+// f = e^(m - to); 0 for terms that vanish, and for none (m = -inf, f = 1).
+__device__ __forceinline__ float shifted(float S, float T, float f, float m, float to) {
+  return f == 0.f || m == -INFINITY ? 0.f : f * (T + (m - to) * S);
+}
+
 // Joins a row's chunks; one workgroup per row.
 template <int TYPE>
 __global__ __launch_bounds__(256) void k_logprobs_join(LogprobArgs a, Parts parts, int chunks) {
@@ -402,29 +439,37 @@ __global__ __launch_bounds__(256) void k_logprobs_join(LogprobArgs a, Parts part
   const int r = blockIdx.x, tid = threadIdx.x, k = a.top_k;
   extern __shared__ u64 keys[];  // [chunks][k]
   const size_t part = (size_t)r * chunks;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   for (int i = tid; i < chunks * k; i += 256) keys[i] = parts.keys[part * k + i];
-  // every thread sums all chunks, in their order
-  RowSums rs{-INFINITY, 0.f, 0.f};
-  for (int c = 0; c < chunks; ++c) rs.m = fmaxf(rs.m, parts.sums[(part + c) * 3]);
-  const float base = rs.base();
-  for (int c = 0; c < chunks; ++c) {
-    const float* p = parts.sums + (part + c) * 3;
-    if (p[0] == -INFINITY) {
-      rs.S += p[1];  // 0, or NaN
-      continue;
-    }
-    const float d = p[0] - base, f = expf(d);
-    rs.S += p[1] * f;
-    rs.T += f == 0.f ? 0.f : f * (p[2] + d * p[1]);
-  }
-  if (tid == 0 && a.entropy) a.entropy[r] = rs.entropy();
-  if (tid < a.n_tokens) {
-    int n = 0;
-    for (int c = 0; c < chunks; ++c) n += parts.counts[(part + c) * a.n_tokens + tid];
-    const size_t at = (size_t)r * a.n_tokens + tid;
-    const int tok = a.tokens[at];
+  int tok = -1;
+  float xt = 0.f;
+  if (lane < a.n_tokens) {
+    tok = a.tokens[(size_t)r * a.n_tokens + lane];
     const void* row = (const uint8_t*)a.x + (size_t)r * a.stride * L::size;
-    write_token(a, at, rs, tok, tok >= 0 && tok < a.vocab ? L::at(row, tok) : 0.f, n);
+    if (tok >= 0 && tok < a.vocab) xt = L::at(row, tok);
+  }
+  // every wave sums all chunks, a lane each
+  float m = -INFINITY, S = 0.f, T = 0.f;
+  for (int c = lane; c < chunks; c += 64) {
+    const float* p = parts.sums + (part + c) * 3;
+    const RowSums one{p[0], p[1], p[2]};
+    const float top = fmaxf(m, one.m), to = top == -INFINITY ? 0.f : top;
+    const float f = m == -INFINITY ? 1.f : expf(m - to), g = one.m == -INFINITY ? 1.f : expf(one.m - to);
+    T = shifted(S, T, f, m, to) + shifted(one.S, one.T, g, one.m, to);
+    S = S * f + one.S * g;
+    m = top;
+  }
+  RowSums rs;
+  rs.m = wave_max(m);
+  const float base = rs.base(), f = m == -INFINITY ? 1.f : expf(m - base);
+  rs.T = wave_sum(shifted(S, T, f, m, base));
+  rs.S = wave_sum(S * f);
+  if (tid == 0 && a.entropy) a.entropy[r] = rs.entropy();
+  for (int t = wave; t < a.n_tokens; t += 4) {
+    int n = 0;
+    for (int c = lane; c < chunks; c += 64) n += parts.counts[(part + c) * a.n_tokens + t];
+    n = wave_sum(n);
+    if (lane == t) write_token(a, (size_t)r * a.n_tokens + t, rs, tok, xt, n);
   }
   __syncthreads();
   // a key's place: its place in its own chunk, and the keys before it in the
@@ -449,14 +494,14 @@ __global__ __launch_bounds__(256) void k_logprobs_join(LogprobArgs a, Parts part
   }
 }
 
-// Chunks of a row: none where a workgroup of up to 1024 threads holds it all
-// (the launch then writes the results itself), else of 256 threads.  A row may
-// start inside a 16-byte block.
+// Chunks of a row: one where a workgroup of up to 1024 threads holds it all (the
+// launch then writes the results itself), else of 256 threads.  skew: logits
+// that may stand before the row's first in its 16-byte block (7 at most).
 struct Plan {
   int waves, chunks;
 };
-Plan plan(int vocab) {
-  const int most = vocab + 7;
+Plan plan(int vocab, int skew) {
+  const int most = vocab + skew;
   for (int w = 4; w <= 16; w *= 2)
     if (most <= w * 64 * kLpVals) return {w, 1};
   return {4, (most + 4 * 64 * kLpVals - 1) / (4 * 64 * kLpVals)};
@@ -467,20 +512,22 @@ size_t align16(size_t n) { return (n + 15) & ~(size_t)15; }
 }  // namespace
 
 bool logprobs_fit(int rows, int vocab) {
-  return vocab <= kLogprobVocab && (int64_t)rows * plan(vocab).chunks <= (1 << 22);
+  return vocab <= kLogprobVocab && (int64_t)rows * plan(vocab, 7).chunks <= (1 << 22);
 }
 
 size_t logprobs_bytes(int rows, int vocab, int n_tokens, int top_k) {
-  const size_t c = (size_t)plan(vocab).chunks * rows;
-  if (plan(vocab).chunks == 1) return 0;
+  const size_t chunks = plan(vocab, 7).chunks, c = chunks * rows;
+  if (chunks == 1) return 0;
   return align16(c * 12) + align16(c * n_tokens * 4) + c * top_k * 8;
 }
 
 template <int TYPE>
 static hipError_t launch_typed(const LogprobArgs& a, uint8_t* ws, hipStream_t s) {
-  const Plan p = plan(a.vocab);
+  constexpr int ES = Logit<TYPE>::size;
+  const bool blocks = (uintptr_t)a.x % 16 == 0 && (a.rows == 1 || a.stride * ES % 16 == 0);
+  const Plan p = plan(a.vocab, blocks ? 0 : 16 / ES - 1);
   Parts parts{};
-  const dim3 grid(p.chunks * a.rows);
+  const dim3 grid(a.rows, p.chunks);
   if (p.chunks > 1) {
     const size_t c = (size_t)p.chunks * a.rows;
     parts.sums = (float*)ws;
