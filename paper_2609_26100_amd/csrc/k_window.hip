@@ -1,64 +1,665 @@
 // Attention with a sliding window and sinks over the paged KV cache (gfx950).
+//
+// A row at position p sees token t when t <= p and (t < sinks or t > p - window).
+// The query heads that share a kv head are rows beside each other (row i of
+// group head j is "virtual" row i * group + j), so that each page is read once
+// for all of them.  A workgroup takes a block of virtual rows of one (sequence,
+// kv head) and walks only the pages that some row of it sees: those of the
+// sinks, then those from the first row's window on.
+//
+// One pass over the pages with the running maximum and sum of the softmax, in
+// powers of two:
+//   * S = K Q^T puts tokens on the MFMA rows and query rows on its columns:
+//     lane (row r16, group grp) holds the scores of tokens 4 grp .. 4 grp + 3 of a
+//     page.  The maximum takes one exchange over the four lanes of a row, the
+//     sums are kept per lane and added at the end.
+//   * O^T = V^T P^T takes the scores' layout as its second operand without
+//     moving them.
+// Two kernels: few rows (up to 16) are bound by the cache's bytes, so each wave
+// streams pages of its own into registers and the waves' states meet at the end;
+// many rows share each page through LDS, a wave for each 16 or 32 rows.  Where
+// the blocks are too few for the chip, each block's pages are split among several workgroups
+// and a second launch joins their states.
+//
+// Tokens that no row of the block sees may hold anything: their scores are
+// replaced, and their V, which the product would multiply by 0, is cleared.
 #include "../../include/tss.h"
 #include "tss_internal.h"
 
+#include <algorithm>
+#include <climits>
+
 namespace tss {
 
-// One wave per (row, query head); a lane holds HD / 64 dimensions.
-template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_window(WindowArgs a) {
-  constexpr int N = HD / 64;
-  const int lane = threadIdx.x & 63;
-  const int qh = blockIdx.y * 4 + (threadIdx.x >> 6), kvh = qh / a.group;
-  if (qh >= a.n_heads * a.group) return;
-  const int s = blockIdx.x / a.max_rows, i = blockIdx.x % a.max_rows;
-  const int r0 = max(a.row_offsets[s], 0), r1 = min(a.row_offsets[s + 1], a.rows);
-  const int r = r0 + i;
-  if (r >= r1) return;
-  const int len = min(min(a.lengths[s], a.max_length), a.table_stride * kPage);
-  const int p = len - (r1 - r0) + i;
-  float q[N], o[N], m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    q[n] = (float)((const T*)a.q)[(size_t)r * a.q_stride + (size_t)qh * HD + lane * N + n] * a.scale_log2;
-    o[n] = 0.f;
-  }
-  for (int t = 0; t <= p; ++t) {
-    if (a.window > 0 && t >= a.sinks && t <= p - a.window) {
-      t = p - a.window;
-      continue;
-    }
-    const int page = a.page_table[(size_t)s * a.table_stride + t / kPage], c = t % kPage;
-    if (page < 0 || page >= a.n_pages) continue;
-    const T* k = (const T*)a.kv_pages + (((size_t)page * 2) * a.n_heads + kvh) * (kPage * HD);
-    const T* v = k + (size_t)a.n_heads * (kPage * HD);
-    float d = 0.f;
-#pragma unroll
-    for (int n = 0; n < N; ++n) d += q[n] * (float)k[c * HD + lane * N + n];
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) d += __shfl_xor(d, off);
-    const float mx = fmaxf(m, d), f = exp2f(m - mx), e = exp2f(d - mx);
-    m = mx;
-    l = l * f + e;
-#pragma unroll
-    for (int n = 0; n < N; ++n) o[n] = o[n] * f + e * (float)v[(c / 4) * HD * 4 + (lane * N + n) * 4 + c % 4];
-  }
-#pragma unroll
-  for (int n = 0; n < N; ++n)
-    ((T*)a.o)[(size_t)r * a.o_stride + (size_t)qh * HD + lane * N + n] = (T)(l > 0.f ? o[n] / l : 0.f);
+namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kMaxSplits = 64;
+constexpr float kLowest = -3e38f;  // running maximum of a row that has seen nothing
+
+// Over the four lanes l, l ^ 16, l ^ 32, l ^ 48 of a row.
+__device__ __forceinline__ float max4(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
+}
+__device__ __forceinline__ float sum4(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(h[0]) + __uint_as_float(h[1]);
 }
 
-hipError_t launch_window(bool f16, int head_dim, const WindowArgs& a, hipStream_t s) {
-  const dim3 grid(a.n_seqs * a.max_rows, (a.n_heads * a.group + 3) / 4);
-  if (f16 && head_dim == 128)
-    TSS_LAUNCH((k_window<_Float16, 128>), grid, dim3(256), 0, s, a);
-  else if (f16)
-    TSS_LAUNCH((k_window<_Float16, 64>), grid, dim3(256), 0, s, a);
-  else if (head_dim == 128)
-    TSS_LAUNCH((k_window<float, 128>), grid, dim3(256), 0, s, a);
-  else
-    TSS_LAUNCH((k_window<float, 64>), grid, dim3(256), 0, s, a);
+// A block of virtual rows of one sequence and the pages it walks.
+struct Block {
+  int r0, rows;          // first row of the sequence, its rows
+  int v0, n_v;           // first virtual row of the block, how many it has (0: nothing to do)
+  int p0;                // position of the sequence's first row (may be negative: more rows than tokens)
+  int lo, hi;            // positions of the block's first and last row, at least -1
+  int sinks, window;
+  int sink_pages, win_page, n_pages;  // page i of the walk: i < sink_pages ? i : win_page + i - sink_pages
+  const int32_t* table;
+
+  __device__ int page(int i) const { return i < sink_pages ? i : win_page + (i - sink_pages); }
+  // position of a virtual row
+  __device__ int pos(int v, int group) const { return max(p0 + v / group, -1); }
+  __device__ bool sees(int t, int p) const { return (t <= p) & ((t < sinks) | (t > p - window)); }
+  // every row from position a to b sees all of the page, resp. none does
+  __device__ bool all_see(int page, int a, int b) const {
+    const int t = page * kPage;
+    return t + kPage - 1 <= a && (t + kPage - 1 < sinks || t > b - window);
+  }
+  __device__ bool none_sees(int page, int a, int b) const {
+    const int t = page * kPage;
+    return t > b || (t >= sinks && t + kPage - 1 <= a - window);
+  }
+  // some row of the block sees the token
+  __device__ bool live(int t) const { return (t <= hi) & ((t < sinks) | (t > lo - window)); }
+};
+
+__device__ __forceinline__ Block make_block(const WindowArgs& a, int s, int first, int most) {
+  Block b{};
+  b.r0 = min(max(a.row_offsets[s], 0), a.rows);
+  b.rows = min(max(a.row_offsets[s + 1], b.r0), a.rows) - b.r0;
+  const int len = max(0, min(min(a.lengths[s], a.max_length), a.table_stride * kPage));
+  b.p0 = len - b.rows;
+  b.v0 = first;
+  b.n_v = max(0, min(most, min(b.rows, a.max_rows) * a.group - first));
+  b.sinks = a.sinks;
+  b.window = a.window > 0 ? a.window : INT_MAX;
+  b.table = a.page_table + (size_t)s * a.table_stride;
+  if (b.n_v == 0) return b;
+  b.lo = b.pos(first, a.group);
+  b.hi = b.pos(first + b.n_v - 1, a.group);
+  if (b.hi < 0) return b;  // no page
+  b.win_page = max(0, max(b.lo, 0) - b.window + 1) / kPage;
+  b.sink_pages = min((b.sinks + kPage - 1) / kPage, b.win_page);
+  b.n_pages = b.sink_pages + b.hi / kPage - b.win_page + 1;
+  return b;
+}
+
+// Words of a lane's V piece (tokens 0, 1 and 2, 3 of its group) that are kept.
+__device__ __forceinline__ uint2 keep16(const Block& b, int t, bool there) {
+  auto half = [&](int u) { return there & b.live(t + u) ? 0xffffu : 0u; };
+  return uint2{half(0) | half(1) << 16, half(2) | half(3) << 16};
+}
+
+__device__ __forceinline__ uint4 both(uint4 a, uint4 b) { return uint4{a.x & b.x, a.y & b.y, a.z & b.z, a.w & b.w}; }
+
+template <typename T, int HD>
+__device__ __forceinline__ const uint8_t* page_k(const WindowArgs& a, int id, int head) {
+  return a.kv_pages + ((size_t)id * 2 * a.n_heads + head) * (kPage * HD * sizeof(T));
+}
+
+__device__ __forceinline__ size_t out_index(const WindowArgs& a, const Block& b, int v, int head, int hd) {
+  return (size_t)(b.r0 + v / a.group) * a.o_stride + (size_t)(head * a.group + v % a.group) * hd;
+}
+// slot of a virtual row's partial state
+__device__ __forceinline__ size_t part_slot(const WindowArgs& a, const Block& b, int v, int head, int split) {
+  return ((size_t)split * a.rows + b.r0 + v / a.group) * (a.n_heads * a.group) + head * a.group + v % a.group;
+}
+
+// --- up to 16 virtual rows ------------------------------------------------------
+
+constexpr int kFewWaves = 8, kFewRows = 16;
+
+// A page in a wave's registers.  Lane (r16, grp): piece c of K holds 16 bytes of
+// token r16 from byte 64 c + 16 grp on; piece i of V holds tokens 4 grp .. + 3 of two
+// (fp16: 32 i + 2 r16, + 1) or one (fp32: 16 i + r16) dimensions.
+template <typename T, int HD>
+struct Page {
+  static constexpr int N = HD * (int)sizeof(T) / 64;
+  uint4 k[N], v[N];
+  int number;   // page of the sequence (scalar)
+  bool there;   // its id is one of the pool's
+
+  __device__ __forceinline__ void load(const WindowArgs& a, int page, int id, int head, int r16, int grp) {
+    number = page;
+    there = (unsigned)id < (unsigned)a.n_pages;
+    const uint8_t* kb = page_k<T, HD>(a, there ? id : 0, head);
+    const uint8_t* vb = kb + (size_t)a.n_heads * (kPage * HD * sizeof(T));
+#pragma unroll
+    for (int c = 0; c < N; ++c) k[c] = *(const uint4*)(kb + (unsigned)(r16 * HD * (int)sizeof(T) + grp * 16 + c * 64));
+#pragma unroll
+    for (int c = 0; c < N; ++c) v[c] = *(const uint4*)(vb + (unsigned)(grp * HD * 4 * (int)sizeof(T) + r16 * 16 + c * 256));
+  }
+};
+
+template <typename T, int HD>
+__device__ __forceinline__ f32x4 scores(const Page<T, HD>& pg, const uint4* q) {
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < Page<T, HD>::N; ++c) {
+    if constexpr (sizeof(T) == 2) {
+      s = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, pg.k[c]), __builtin_bit_cast(f16x8, q[c]), s,
+                                                 0, 0, 0);
+    } else {
+      const f32x4 x = __builtin_bit_cast(f32x4, pg.k[c]), y = __builtin_bit_cast(f32x4, q[c]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], s, 0, 0, 0);
+    }
+  }
+  return s;
+}
+
+// Outputs of a lane: o[n][v] is dimension dim_of(n, v) of row r16.
+template <typename T>
+__device__ __forceinline__ int dim_of(int n, int v, int grp) {
+  if constexpr (sizeof(T) == 2) return 32 * (n >> 1) + 8 * grp + 2 * v + (n & 1);
+  return 16 * n + 4 * grp + v;
+}
+
+// grid (kv head + heads * block, sequence, split)
+template <typename T, int HD>
+__global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(WindowArgs a, int splits, float* part_o,
+                                                                  float* part_ml) {
+  constexpr int PP = sizeof(T) == 2 ? 2 : 1;  // pages of a step
+  constexpr int N = Page<T, HD>::N, NO = HD / 16;
+  constexpr int LD = 64 + 4;
+  __shared__ float s_o[kFewWaves][kFewRows][LD];
+  __shared__ float s_m[kFewWaves][kFewRows], s_l[kFewWaves][kFewRows];
+  const int head = blockIdx.x % a.n_heads;
+  const Block b = make_block(a, blockIdx.y, blockIdx.x / a.n_heads * kFewRows, kFewRows);
+  if (b.n_v == 0) return;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int r16 = lane & 15, grp = lane >> 4;
+  const int row = b.v0 + min(r16, b.n_v - 1);      // lanes past the block's rows do the last one again
+  const int pos = b.pos(row, a.group);
+
+  // this split's pages, from `from`; wave w takes steps w, w + 8, ...
+  const int steps = (b.n_pages + PP - 1) / PP, per = (steps + splits - 1) / splits;
+  const int st0 = blockIdx.z * per, n_st = min(per, steps - st0);
+  int ids = 0;
+  auto walk = [&](int st, int p) { return (st0 + st) * PP + p; };  // page p of this split's step st
+  auto load_ids = [&](int st) {  // of this wave's 64 / PP steps from st on
+    const int i = walk(st + lane / PP * kFewWaves, lane % PP);
+    ids = b.table[b.page(min(i, b.n_pages - 1))];
+  };
+  uint4 q[N];
+  {
+    const T* qr = (const T*)a.q + (size_t)(b.r0 + row / a.group) * a.q_stride +
+                  (size_t)(head * a.group + row % a.group) * HD;
+#pragma unroll
+    for (int c = 0; c < N; ++c) q[c] = *(const uint4*)((const uint8_t*)qr + c * 64 + grp * 16);
+  }
+  f32x4 o[NO];
+#pragma unroll
+  for (int n = 0; n < NO; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = kLowest, l = 0.f;
+
+  Page<T, HD> buf[2][PP];
+  auto fetch = [&](Page<T, HD>* pg, int st) {
+    if (((st - wave) / kFewWaves) % (64 / PP) == 0) load_ids(st);
+    const int j = ((st - wave) / kFewWaves) % (64 / PP) * PP;
+#pragma unroll
+    for (int p = 0; p < PP; ++p) {
+      const int i = walk(st, p);
+      const int id = __builtin_amdgcn_readlane(ids, j + p);
+      pg[p].load(a, b.page(min(i, b.n_pages - 1)), i < b.n_pages ? id : -1, head, r16, grp);
+    }
+  };
+  auto compute = [&](Page<T, HD>* pg) {
+    f32x4 S[PP];
+    bool whole = true;
+#pragma unroll
+    for (int p = 0; p < PP; ++p) {
+      S[p] = scores<T, HD>(pg[p], q);
+      if (!pg[p].there || !b.all_see(pg[p].number, b.lo, b.hi)) {
+        whole = false;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const bool seen = pg[p].there & b.sees(pg[p].number * kPage + 4 * grp + v, pos);
+          S[p][v] = seen ? S[p][v] : -INFINITY;
+        }
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int p = 0; p < PP; ++p)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) mx = fmaxf(mx, S[p][v]);
+    mx = max4(fmaxf(m, mx * a.scale_log2));
+    const float alpha = __builtin_amdgcn_exp2f(m - mx);
+    m = mx;
+    float sum = 0.f;
+#pragma unroll
+    for (int p = 0; p < PP; ++p)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        S[p][v] = __builtin_amdgcn_exp2f(S[p][v] * a.scale_log2 - mx);
+        sum += S[p][v];
+      }
+    l = l * alpha + sum;
+    if (__any(alpha != 1.f)) {
+#pragma unroll
+      for (int n = 0; n < NO; ++n) o[n] *= alpha;
+    }
+    if (!whole) {
+#pragma unroll
+      for (int p = 0; p < PP; ++p) {
+        const int t = pg[p].number * kPage + 4 * grp;
+        if constexpr (sizeof(T) == 2) {
+          const uint2 k = keep16(b, t, pg[p].there);
+#pragma unroll
+          for (int i = 0; i < N; ++i) pg[p].v[i] = both(pg[p].v[i], uint4{k.x, k.y, k.x, k.y});
+        } else {
+          auto word = [&](int u) { return pg[p].there & b.live(t + u) ? ~0u : 0u; };
+          const uint4 k = {word(0), word(1), word(2), word(3)};
+#pragma unroll
+          for (int i = 0; i < N; ++i) pg[p].v[i] = both(pg[p].v[i], k);
+        }
+      }
+    }
+    if constexpr (sizeof(T) == 2) {
+      // k = 8 grp + 4 p + u is token 4 grp + u of page p
+      f16x8 P;
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) P[4 * p + v] = (_Float16)S[p][v];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const uint4 va = pg[0].v[i], vb = pg[PP - 1].v[i];
+        o[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, uint4{va.x, va.y, vb.x, vb.y}), P,
+                                                          o[2 * i], 0, 0, 0);
+        o[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, uint4{va.z, va.w, vb.z, vb.w}),
+                                                              P, o[2 * i + 1], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const f32x4 x = __builtin_bit_cast(f32x4, pg[0].v[i]);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[v], S[0][v], o[i], 0, 0, 0);
+      }
+    }
+  };
+
+  if (wave < n_st) {
+    fetch(buf[0], wave);
+    for (int st = wave; st < n_st; st += 2 * kFewWaves) {
+      if (st + kFewWaves < n_st) fetch(buf[1], st + kFewWaves);
+      compute(buf[0]);
+      if (st + kFewWaves >= n_st) break;
+      if (st + 2 * kFewWaves < n_st) fetch(buf[0], st + 2 * kFewWaves);
+      compute(buf[1]);
+    }
+  }
+
+  // the waves' states meet, 64 dimensions at a time
+  l = sum4(l);
+  if (grp == 0) {
+    s_m[wave][r16] = m;
+    s_l[wave][r16] = l;
+  }
+  const int orow = tid >> 5, od = (tid & 31) * 2;  // a thread's two outputs of a round
+#pragma unroll
+  for (int h = 0; h < HD / 64; ++h) {
+    if (h) __syncthreads();
+#pragma unroll
+    for (int n = 4 * h; n < 4 * h + 4; ++n)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) s_o[wave][r16][dim_of<T>(n, v, grp) - 64 * h] = o[n][v];
+    __syncthreads();
+    float top = kLowest;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, s_m[w][orow]);
+    float L = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(s_m[w][orow] - top);
+      const float2 p = *(const float2*)&s_o[w][orow][od];
+      L += f * s_l[w][orow];
+      x += f * p.x;
+      y += f * p.y;
+    }
+    if (orow < b.n_v) {
+      const int v = b.v0 + orow;
+      if (splits > 1) {
+        const size_t slot = part_slot(a, b, v, head, blockIdx.z);
+        *(float2*)(part_o + slot * HD + 64 * h + od) = make_float2(x, y);
+        if (h == 0 && od == 0) *(float2*)(part_ml + slot * 2) = make_float2(top, L);
+      } else {
+        const float inv = L > 0.f ? 1.f / L : L;  // 0 for a row that sees nothing, NaN stays
+        T* to = (T*)a.o + out_index(a, b, v, head, HD) + 64 * h + od;
+        to[0] = (T)(x * inv);
+        to[1] = (T)(y * inv);
+      }
+    }
+  }
+}
+
+// --- many rows (fp16) --------------------------------------------------------------
+
+constexpr int kRowsWaves = 4, kRowsPages = 4, kRowsStages = 2;
+
+// Four waves of TILES 16-row tiles walk the pages together, four pages a step,
+// one loaded by each wave into an LDS ring by global -> LDS loads, two steps in flight.
+// K chunk c covers dims 32 c .. + 31 (16 tokens x 64 bytes of a page), V chunk i
+// dims 32 i .. + 31 of four token groups (4 x 256 bytes): each is one KiB load, read
+// back lane by lane in order.  grid as k_window_few.
+template <int HD, int TILES>
+__global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(WindowArgs a, int splits, int blocks,
+                                                                    float* part_o, float* part_ml) {
+  constexpr int NK = HD / 32;              // KiB of a K (or V) page block
+  constexpr int PW = 2 * NK;               // loads of one wave per step: one page
+  constexpr int STAGE = kRowsPages * 2 * NK * 1024;
+  constexpr int ROWS = kRowsWaves * TILES * 16;
+  __shared__ __align__(16) uint8_t ring[kRowsStages * STAGE];
+  const int head = blockIdx.x % a.n_heads;
+  // the last rows first: without a window theirs is the longest walk
+  const Block b = make_block(a, blockIdx.y, (blocks - 1 - (int)blockIdx.x / a.n_heads) * ROWS, ROWS);
+  if (b.n_v == 0) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int r16 = lane & 15, grp = lane >> 4;
+  const int steps = (b.n_pages + kRowsPages - 1) / kRowsPages, per = (steps + splits - 1) / splits;
+  const int st0 = blockIdx.z * per, n_st = max(0, min(per, steps - st0));
+  const int w0 = wave * TILES * 16;                         // the wave's first row of the block
+  const bool on = w0 < b.n_v;
+  const int wlo = b.pos(b.v0 + w0, a.group), whi = b.pos(b.v0 + min(w0 + TILES * 16, b.n_v) - 1, a.group);
+
+  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)ring;
+  const unsigned koff = (unsigned)(r16 * HD * 2 + grp * 16);          // + c * 64
+  const unsigned voff = (unsigned)(grp * HD * 8 + r16 * 16);          // + i * 256
+  int ids = 0;  // lane l: id of page l of sixteen steps, -1 past the walk
+  auto load_ids = [&](int st) {
+    const int i = (st0 + st) * kRowsPages + lane;
+    const int id = b.table[b.page(min(i, b.n_pages - 1))];
+    ids = i < b.n_pages && (unsigned)id < (unsigned)a.n_pages ? id : -1;
+  };
+  auto issue = [&](int st) {
+    const int phys = max(0, __builtin_amdgcn_readlane(ids, (st * kRowsPages + wave) & 63));
+    const uint8_t* kb = page_k<_Float16, HD>(a, phys, head);
+    const uint8_t* vb = kb + (size_t)a.n_heads * (kPage * HD * 2);
+    const unsigned dst = lds0 + (unsigned)((st % kRowsStages) * STAGE + wave * 2 * NK * 1024);
+#pragma unroll
+    for (int c = 0; c < NK; ++c) dma_kib(kb, koff + c * 64u, dst + c * 1024u);
+#pragma unroll
+    for (int c = 0; c < NK; ++c) dma_kib(vb, voff + c * 256u, dst + (NK + c) * 1024u);
+  };
+
+  f16x8 q[TILES][NK];
+  int pos[TILES];
+  f32x4 O[TILES][2 * NK];  // [2 i + j]: dims 32 i + 8 grp + 2 v + j
+  float m_run[TILES], l_run[TILES];
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) {
+    const int v = b.v0 + min(w0 + t * 16 + r16, b.n_v - 1);
+    pos[t] = b.pos(v, a.group);
+    const _Float16* qr = (const _Float16*)a.q + (size_t)(b.r0 + v / a.group) * a.q_stride +
+                         (size_t)(head * a.group + v % a.group) * HD + grp * 8;
+#pragma unroll
+    for (int c = 0; c < NK; ++c) q[t][c] = *(const f16x8*)(qr + c * 32);
+    m_run[t] = kLowest;
+    l_run[t] = 0.f;
+#pragma unroll
+    for (int n = 0; n < 2 * NK; ++n) O[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  if (n_st > 0) {
+    load_ids(0);
+    issue(0);
+  }
+  for (int st = 0; st < n_st; ++st) {
+    const int here = ids;  // the ids of step st (the next step may load others)
+    if (st + 1 < n_st) {
+      if (((st + 1) & 15) == 0) load_ids(st + 1);
+      issue(st + 1);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PW) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    __builtin_amdgcn_s_barrier();  // every wave's page of step st has landed
+    asm volatile("" ::: "memory");
+    int number[kRowsPages];
+    bool there[kRowsPages], any = false, whole = true;
+#pragma unroll
+    for (int p = 0; p < kRowsPages; ++p) {
+      there[p] = __builtin_amdgcn_readlane(here, (st * kRowsPages + p) & 63) >= 0;
+      number[p] = b.page(min((st0 + st) * kRowsPages + p, b.n_pages - 1));
+      any |= there[p] && !b.none_sees(number[p], wlo, whi);
+      whole &= there[p] && b.all_see(number[p], wlo, whi);
+    }
+    if (on && any) {
+      const uint8_t* base = ring + (st % kRowsStages) * STAGE + lane * 16;
+      f16x8 P[TILES][2];
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        f32x4 S[kRowsPages];
+#pragma unroll
+        for (int p = 0; p < kRowsPages; ++p) {
+          S[p] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < NK; ++c)
+            S[p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*(const f16x8*)(base + (p * 2 * NK + c) * 1024), q[t][c],
+                                                          S[p], 0, 0, 0);
+        }
+        if (!whole) {
+#pragma unroll
+          for (int p = 0; p < kRowsPages; ++p)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const bool seen = there[p] & b.sees(number[p] * kPage + 4 * grp + v, pos[t]);
+              S[p][v] = seen ? S[p][v] : -INFINITY;  // a select, no branch
+            }
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int p = 0; p < kRowsPages; ++p)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) mx = fmaxf(mx, S[p][v]);
+        mx = max4(fmaxf(m_run[t], mx * a.scale_log2));
+        const float alpha = __builtin_amdgcn_exp2f(m_run[t] - mx);
+        m_run[t] = mx;
+        float l = 0.f;
+#pragma unroll
+        for (int p = 0; p < kRowsPages; ++p)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const float e = __builtin_amdgcn_exp2f(S[p][v] * a.scale_log2 - mx);
+            l += e;
+            P[t][p >> 1][(p & 1) * 4 + v] = (_Float16)e;
+          }
+        l_run[t] = l_run[t] * alpha + l;
+        if (__any(alpha != 1.f)) {  // most steps raise no row's maximum
+#pragma unroll
+          for (int n = 0; n < 2 * NK; ++n) O[t][n] *= alpha;
+        }
+      }
+      // two pages per MFMA: k = 8 grp + 4 b + u is token 4 grp + u of page 2 h + b
+#pragma unroll
+      for (int h = 0; h < kRowsPages / 2; ++h) {
+        uint2 ka = {~0u, ~0u}, kb = {~0u, ~0u};
+        if (!whole) {
+          ka = keep16(b, number[2 * h] * kPage + 4 * grp, there[2 * h]);
+          kb = keep16(b, number[2 * h + 1] * kPage + 4 * grp, there[2 * h + 1]);
+        }
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+          const uint4 va = *(const uint4*)(base + (4 * h * NK + NK + i) * 1024);
+          const uint4 vb = *(const uint4*)(base + ((4 * h + 2) * NK + NK + i) * 1024);
+          const f16x8 v0 = __builtin_bit_cast(f16x8, uint4{va.x & ka.x, va.y & ka.y, vb.x & kb.x, vb.y & kb.y});
+          const f16x8 v1 = __builtin_bit_cast(f16x8, uint4{va.z & ka.x, va.w & ka.y, vb.z & kb.x, vb.w & kb.y});
+#pragma unroll
+          for (int t = 0; t < TILES; ++t) {
+            O[t][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, P[t][h], O[t][2 * i], 0, 0, 0);
+            O[t][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, P[t][h], O[t][2 * i + 1], 0, 0, 0);
+          }
+        }
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();  // step st has been read: its slot may be refilled
+    asm volatile("" ::: "memory");
+  }
+
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) {
+    const int i = w0 + t * 16 + r16;
+    const float l = sum4(l_run[t]);
+    if (i >= b.n_v) continue;
+    const int v = b.v0 + i;
+    if (splits > 1) {
+      const size_t slot = part_slot(a, b, v, head, blockIdx.z);
+#pragma unroll
+      for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          *(float4*)(part_o + slot * HD + 32 * n + 8 * grp + 4 * e) =
+              make_float4(O[t][2 * n][2 * e], O[t][2 * n + 1][2 * e], O[t][2 * n][2 * e + 1], O[t][2 * n + 1][2 * e + 1]);
+      if (grp == 0) *(float2*)(part_ml + slot * 2) = make_float2(m_run[t], l);
+      continue;
+    }
+    const float inv = l > 0.f ? 1.f / l : l;
+    _Float16* to = (_Float16*)a.o + out_index(a, b, v, head, HD) + 8 * grp;
+#pragma unroll
+    for (int n = 0; n < NK; ++n) {
+      f16x8 x;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        x[2 * u] = (_Float16)(O[t][2 * n][u] * inv);
+        x[2 * u + 1] = (_Float16)(O[t][2 * n + 1][u] * inv);
+      }
+      *(f16x8*)(to + 32 * n) = x;
+    }
+  }
+}
+
+// Joins the splits' states, a workgroup for each (row, query head), a quarter of
+// the splits for each of its waves.  grid (rows of a sequence, sequence, query head).
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_window_join(WindowArgs a, int splits, const float* part_o,
+                                                     const float* part_ml) {
+  constexpr int N = HD / 64;
+  __shared__ float s_o[4][HD];
+  const int s = blockIdx.y, qh = blockIdx.z, heads = a.n_heads * a.group;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int r0 = min(max(a.row_offsets[s], 0), a.rows), r1 = min(max(a.row_offsets[s + 1], r0), a.rows);
+  const int row = r0 + blockIdx.x;
+  if (row >= r1) return;
+  const size_t slot = (size_t)row * heads + qh, stride = (size_t)a.rows * heads;
+  float2 ml = make_float2(kLowest, 0.f);
+  if (lane < splits) ml = *(const float2*)(part_ml + (slot + lane * stride) * 2);
+  float p[kMaxSplits / 4][N];
+#pragma unroll
+  for (int i = 0; i < kMaxSplits / 4; ++i) {
+    const int g = min(wave + 4 * i, splits - 1);
+    if (4 * i >= splits) break;
+#pragma unroll
+    for (int n = 0; n < N; ++n) p[i][n] = part_o[(slot + g * stride) * HD + lane * N + n];
+  }
+  float top = ml.x, L;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+  const float f = __builtin_amdgcn_exp2f(ml.x - top);
+  L = f * ml.y;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) L += __shfl_xor(L, off);
+  float o[N] = {};
+#pragma unroll
+  for (int i = 0; i < kMaxSplits / 4; ++i) {
+    const int g = wave + 4 * i;
+    if (g >= splits) break;
+    const float w = __shfl(f, g);
+#pragma unroll
+    for (int n = 0; n < N; ++n) o[n] += w * p[i][n];
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) s_o[wave][lane * N + n] = o[n];
+  __syncthreads();
+  if (threadIdx.x < HD) {
+    const int d = threadIdx.x;
+    const float x = (s_o[0][d] + s_o[1][d]) + (s_o[2][d] + s_o[3][d]);
+    ((T*)a.o)[(size_t)row * a.o_stride + (size_t)qh * HD + d] = (T)(x * (L > 0.f ? 1.f / L : L));
+  }
+}
+
+// How a call is cut up: virtual rows of a block, blocks of a sequence, splits of
+// a block's pages.  Splits are worth their second launch where the
+// blocks leave most of the chip idle and each still has some pages to walk.
+struct Plan {
+  int rows, blocks, splits;
+};
+Plan plan(bool f16, int n_heads, int group, int n_seqs, int max_rows, int max_length, int sinks, int window) {
+  const int64_t v = (int64_t)max_rows * group;
+  Plan p;
+  p.rows = !f16 || v <= kFewRows ? kFewRows : v <= kRowsWaves * 16 ? kRowsWaves * 16 : kRowsWaves * 32;
+  p.blocks = (int)((v + p.rows - 1) / p.rows);
+  // pages of the longest walk
+  const int64_t block_rows = std::min<int64_t>(max_rows, (p.rows + group - 1) / group + 1);
+  int64_t pages = (max_length + kPage - 1) / kPage;
+  if (window > 0)
+    pages = std::min<int64_t>(pages, (sinks + kPage - 1) / kPage + (window + block_rows + 2 * kPage - 3) / kPage);
+  const int64_t wgs = (int64_t)n_heads * n_seqs * p.blocks;
+  const bool few = p.rows == kFewRows;
+  const int64_t target = few ? 256 : 512, least = few ? 32 : 16;
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, target / std::max<int64_t>(1, wgs), pages / least}));
+  return p;
+}
+
+}  // namespace
+
+bool window_fits(int n_heads, int group, int n_seqs, int max_rows) {
+  // grids: (heads * blocks, sequences, splits) and (rows, sequences, query heads)
+  return n_seqs <= 65535 && (int64_t)n_heads * group <= 65535 &&
+         (int64_t)max_rows * group / kFewRows * n_heads < (1 << 22);
+}
+
+size_t window_bytes(bool f16, int head_dim, int n_heads, int group, int n_seqs, int rows, int max_rows, int max_length,
+                    int sinks, int window) {
+  const Plan p = plan(f16, n_heads, group, n_seqs, max_rows, max_length, sinks, window);
+  return p.splits == 1 ? 0 : (size_t)p.splits * rows * n_heads * group * (head_dim + 2) * 4;
+}
+
+template <typename T, int HD>
+static hipError_t launch_typed(const WindowArgs& a, float* ws, hipStream_t s) {
+  const Plan p = plan(sizeof(T) == 2, a.n_heads, a.group, a.n_seqs, a.max_rows, a.max_length, a.sinks, a.window);
+  float* part_o = ws;
+  float* part_ml = ws + (size_t)p.splits * a.rows * a.n_heads * a.group * HD;
+  const dim3 grid(a.n_heads * p.blocks, a.n_seqs, p.splits);
+  if (p.rows == kFewRows) {
+    TSS_LAUNCH((k_window_few<T, HD>), grid, dim3(kFewWaves * 64), 0, s, a, p.splits, part_o, part_ml);
+  } else if constexpr (sizeof(T) == 2) {
+    if (p.rows == kRowsWaves * 16)
+      TSS_LAUNCH((k_window_rows<HD, 1>), grid, dim3(kRowsWaves * 64), 0, s, a, p.splits, p.blocks, part_o, part_ml);
+    else
+      TSS_LAUNCH((k_window_rows<HD, 2>), grid, dim3(kRowsWaves * 64), 0, s, a, p.splits, p.blocks, part_o, part_ml);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  TSS_LAUNCH((k_window_join<T, HD>), dim3(a.max_rows, a.n_seqs, a.n_heads * a.group), dim3(256), 0, s, a,
+             p.splits, part_o, part_ml);
   return hipGetLastError();
+}
+
+hipError_t launch_window(bool f16, int head_dim, const WindowArgs& a, void* workspace, hipStream_t s) {
+  float* ws = (float*)workspace;
+  if (f16) return head_dim == 128 ? launch_typed<_Float16, 128>(a, ws, s) : launch_typed<_Float16, 64>(a, ws, s);
+  return head_dim == 128 ? launch_typed<float, 128>(a, ws, s) : launch_typed<float, 64>(a, ws, s);
 }
 
 }  // namespace tss

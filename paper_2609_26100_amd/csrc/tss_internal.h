@@ -454,7 +454,10 @@ struct WindowArgs {
   int sinks, window;
   float scale_log2;        // log2(e) * scale
 };
-hipError_t launch_window(bool f16, int head_dim, const WindowArgs& a, hipStream_t s);
+bool window_fits(int n_heads, int group, int n_seqs, int max_rows);  // whether its workgroups can be launched
+size_t window_bytes(bool f16, int head_dim, int n_heads, int group, int n_seqs, int rows, int max_rows, int max_length,
+                    int sinks, int window);
+hipError_t launch_window(bool f16, int head_dim, const WindowArgs& a, void* workspace, hipStream_t s);
 
 constexpr int kCopyPairs = 480;  // page copies of one launch (by value)
 struct CopyArgs {

@@ -48,6 +48,18 @@ const char* kv_fault(const tss_paged_kv* kv) {
   return nullptr;
 }
 
+const char* window_fault(const tss_paged_kv* kv, int32_t n_q_heads, int32_t rows, int32_t max_rows, int32_t max_length,
+                         int32_t sinks, int32_t window) {
+  if (kv->n_seqs < 0 || kv->table_stride < 1 || kv->table_stride > INT32_MAX / kPage) return "bad page table";
+  if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads) return "n_q_heads must be a multiple of n_kv_heads";
+  if (rows < 0 || max_rows < 0 || max_length < 0 || sinks < 0 || window < 0)
+    return "negative rows, length, sinks or window";
+  if (sinks > INT32_MAX - kPage) return "too many sinks";
+  if (!window_fits(kv->n_kv_heads, n_q_heads / kv->n_kv_heads, kv->n_seqs, std::min(max_rows, rows)))
+    return "too many sequences, heads or rows for one launch";
+  return nullptr;
+}
+
 size_t page_bytes(const tss_paged_kv* kv) {
   return (size_t)2 * kv->n_kv_heads * kPage * kv->head_dim * type_size(kv->type);
 }
@@ -92,7 +104,14 @@ int tss_token_logprobs(void* hip_stream, const void* logits, int32_t type, int64
   return launched(launch_logprobs(a, workspace, (hipStream_t)hip_stream), me);
 }
 
-size_t tss_window_attn_bytes(const tss_paged_kv*, int32_t, int32_t, int32_t, int32_t, int32_t, int32_t) { return 0; }
+size_t tss_window_attn_bytes(const tss_paged_kv* kv, int32_t n_q_heads, int32_t rows, int32_t max_rows,
+                             int32_t max_length, int32_t sinks, int32_t window) {
+  if (kv_fault(kv) || window_fault(kv, n_q_heads, rows, max_rows, max_length, sinks, window)) return 0;
+  max_rows = std::min(max_rows, rows);
+  if (max_rows == 0 || kv->n_seqs == 0) return 0;
+  return window_bytes(kv->type == TSS_T_F16, kv->head_dim, kv->n_kv_heads, n_q_heads / kv->n_kv_heads, kv->n_seqs, rows,
+                      max_rows, std::min(max_length, kv->table_stride * kPage), sinks, window);
+}
 
 int tss_window_attn(void* hip_stream, const tss_paged_kv* kv, int32_t layer, const void* q, int64_t q_stride,
                     int32_t n_q_heads, const int32_t* row_offsets, const int32_t* lengths, int32_t rows,
@@ -101,10 +120,8 @@ int tss_window_attn(void* hip_stream, const tss_paged_kv* kv, int32_t layer, con
   const char* me = "tss_window_attn";
   if (const char* f = kv_fault(kv)) return refuse(TSS_EINVAL, me, f);
   if (layer < 0 || layer >= kv->n_layers) return refuse(TSS_EINVAL, me, "no such layer");
-  if (kv->n_seqs < 0 || kv->table_stride < 1) return refuse(TSS_EINVAL, me, "bad page table");
-  if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads) return refuse(TSS_EINVAL, me, "n_q_heads must be a multiple of n_kv_heads");
-  if (rows < 0 || max_rows < 0 || max_length < 0 || sinks < 0 || window < 0)
-    return refuse(TSS_EINVAL, me, "negative rows, length, sinks or window");
+  if (const char* f = window_fault(kv, n_q_heads, rows, max_rows, max_length, sinks, window))
+    return refuse(TSS_EINVAL, me, f);
   if (!(scale >= 0.f) || std::isinf(scale)) return refuse(TSS_EINVAL, me, "scale must be finite and not negative");
   const int64_t width = (int64_t)n_q_heads * kv->head_dim;
   if (rows == 0 || max_rows == 0 || kv->n_seqs == 0) return TSS_OK;
@@ -113,6 +130,8 @@ int tss_window_attn(void* hip_stream, const tss_paged_kv* kv, int32_t layer, con
   if (!q || !out || !row_offsets || !lengths || !kv->page_table) return refuse(TSS_EINVAL, me, "null tensor");
   if (!aligned(q, 16) || !aligned(out, 16)) return refuse(TSS_EINVAL, me, "q and out must be aligned to 16 bytes");
   const size_t need = tss_window_attn_bytes(kv, n_q_heads, rows, max_rows, max_length, sinks, window);
+  max_rows = std::min(max_rows, rows);
+  max_length = std::min(max_length, kv->table_stride * kPage);
   if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16)))
     return refuse(TSS_ENOSPACE, me, "workspace smaller than tss_window_attn_bytes() or not aligned to 16 bytes");
   WindowArgs a{};
@@ -135,7 +154,7 @@ int tss_window_attn(void* hip_stream, const tss_paged_kv* kv, int32_t layer, con
   a.sinks = sinks;
   a.window = window;
   a.scale_log2 = (float)(1.4426950408889634 * (scale > 0.f ? (double)scale : 1.0 / std::sqrt((double)kv->head_dim)));
-  return launched(launch_window(kv->type == TSS_T_F16, kv->head_dim, a, (hipStream_t)hip_stream), me);
+  return launched(launch_window(kv->type == TSS_T_F16, kv->head_dim, a, workspace, (hipStream_t)hip_stream), me);
 }
 
 int tss_copy_pages(void* hip_stream, const tss_paged_kv* kv, const int32_t* src, const int32_t* dst, int32_t n) {
