@@ -39,6 +39,11 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMaxSplits = 64;
 constexpr float kLowest = -3e38f;  // running maximum of a row that has seen nothing
+// A row's reference maximum is raised where the scores exceed it by this (in
+// powers of two): probabilities up to 2^8 of the largest fit fp16 as well as
+// those up to 1 (their rounding is relative), and almost no step has to rescale
+// its outputs, where with a threshold of 0 some row of sixteen nearly always rises.
+constexpr float kRise = 8.f;
 
 // Over the four lanes l, l ^ 16, l ^ 32, l ^ 48 of a row.
 __device__ __forceinline__ float max4(float x) {
@@ -77,6 +82,8 @@ struct Block {
     const int t = page * kPage;
     return t > b || (t >= sinks && t + kPage - 1 <= a - window);
   }
+  // the walk's place of a page from win_page on
+  __device__ int place(int page) const { return page - win_page + sink_pages; }
   // some row of the block sees the token
   __device__ bool live(int t) const { return (t <= hi) & ((t < sinks) | (t > lo - window)); }
 };
@@ -101,6 +108,20 @@ __device__ __forceinline__ Block make_block(const WindowArgs& a, int s, int firs
   b.n_pages = b.sink_pages + b.hi / kPage - b.win_page + 1;
   return b;
 }
+
+// What rows of positions a to b (at least -1) see of a walk, by places: pages
+// first .. last hold some token of their windows, of all_first .. all_last all see
+// all.  Pages of sinks come besides: the walk begins with them, so that page i
+// of the sequence is at place i.
+struct Span {
+  int first, last, all_first, all_last;
+  __device__ Span(const Block& w, int a, int b) {
+    first = w.place(max(0, a - w.window + 1) / kPage);
+    last = b < 0 ? -1 : w.place(b / kPage);
+    all_first = w.place(b - w.window < 0 ? 0 : (b - w.window) / kPage + 1);
+    all_last = w.place((a + 1) / kPage - 1);
+  }
+};
 
 // Words of a lane's V piece (tokens 0, 1 and 2, 3 of its group) that are kept.
 __device__ __forceinline__ uint2 keep16(const Block& b, int t, bool there) {
@@ -381,18 +402,27 @@ __global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(WindowArgs a
   const int w0 = wave * TILES * 16;                         // the wave's first row of the block
   const bool on = w0 < b.n_v;
   const int wlo = b.pos(b.v0 + w0, a.group), whi = b.pos(b.v0 + min(w0 + TILES * 16, b.n_v) - 1, a.group);
+  const Span span(b, wlo, whi);
+  // pages that the sinks fill, and pages of whose tokens each is seen by some row
+  // of the block: its first row's from the window's start, its last row's to the end
+  const int full_sinks = b.sinks / kPage, sink_end = (b.sinks + kPage - 1) / kPage;
+  const int live_first = b.place(b.lo - b.window < 0 ? 0 : (b.lo - b.window) / kPage + 1);
+  const int live_last = b.place((b.hi + 1) / kPage - 1);
 
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)ring;
   const unsigned koff = (unsigned)(r16 * HD * 2 + grp * 16);          // + c * 64
   const unsigned voff = (unsigned)(grp * HD * 8 + r16 * 16);          // + i * 256
-  int ids = 0;  // lane l: id of page l of sixteen steps, -1 past the walk
+  int ids = 0;  // lane l: id of page l of sixteen steps
+  uint64_t good = 0;  // bit l: it is a page of the walk and of the pool
   auto load_ids = [&](int st) {
     const int i = (st0 + st) * kRowsPages + lane;
     const int id = b.table[b.page(min(i, b.n_pages - 1))];
-    ids = i < b.n_pages && (unsigned)id < (unsigned)a.n_pages ? id : -1;
+    const bool there = i < b.n_pages && (unsigned)id < (unsigned)a.n_pages;
+    good = __ballot(there);
+    ids = there ? id : 0;
   };
   auto issue = [&](int st) {
-    const int phys = max(0, __builtin_amdgcn_readlane(ids, (st * kRowsPages + wave) & 63));
+    const int phys = __builtin_amdgcn_readlane(ids, (st * kRowsPages + wave) & 63);
     const uint8_t* kb = page_k<_Float16, HD>(a, phys, head);
     const uint8_t* vb = kb + (size_t)a.n_heads * (kPage * HD * 2);
     const unsigned dst = lds0 + (unsigned)((st % kRowsStages) * STAGE + wave * 2 * NK * 1024);
@@ -425,96 +455,106 @@ __global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(WindowArgs a
     issue(0);
   }
   for (int st = 0; st < n_st; ++st) {
-    const int here = ids;  // the ids of step st (the next step may load others)
+    const unsigned there = (unsigned)(good >> ((st * kRowsPages) & 63)) & ((1u << kRowsPages) - 1);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();  // every wave's page of step st has landed, and step st - 1 has been read
+    asm volatile("" ::: "memory");
     if (st + 1 < n_st) {
       if (((st + 1) & 15) == 0) load_ids(st + 1);
       issue(st + 1);
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PW) : "memory");
-    } else {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
-    __builtin_amdgcn_s_barrier();  // every wave's page of step st has landed
-    asm volatile("" ::: "memory");
-    int number[kRowsPages];
-    bool there[kRowsPages], any = false, whole = true;
-#pragma unroll
-    for (int p = 0; p < kRowsPages; ++p) {
-      there[p] = __builtin_amdgcn_readlane(here, (st * kRowsPages + p) & 63) >= 0;
-      number[p] = b.page(min((st0 + st) * kRowsPages + p, b.n_pages - 1));
-      any |= there[p] && !b.none_sees(number[p], wlo, whi);
-      whole &= there[p] && b.all_see(number[p], wlo, whi);
-    }
+    // some token is seen by a row of the wave; all by all of them; each by some row of the block
+    const int i0 = (st0 + st) * kRowsPages, i1 = i0 + kRowsPages - 1;
+    const bool any = i0 <= span.last && (i0 < sink_end || i1 >= span.first);
+    const bool all_there = there == (1u << kRowsPages) - 1, in_sinks = i1 < full_sinks;
+    const bool whole = all_there && i1 <= span.all_last && (in_sinks || i0 >= span.all_first);
+    const bool clean = all_there && i1 <= live_last && (in_sinks || i0 >= live_first);
     if (on && any) {
       const uint8_t* base = ring + (st % kRowsStages) * STAGE + lane * 16;
       f16x8 P[TILES][2];
+      f32x4 S[TILES][kRowsPages];
 #pragma unroll
-      for (int t = 0; t < TILES; ++t) {
-        f32x4 S[kRowsPages];
+      for (int p = 0; p < kRowsPages; ++p) {
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) S[t][p] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < NK; ++c) {
+          const f16x8 k = *(const f16x8*)(base + (p * 2 * NK + c) * 1024);
+#pragma unroll
+          for (int t = 0; t < TILES; ++t) S[t][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[t][c], S[t][p], 0, 0, 0);
+        }
+      }
+      if (!whole) {
 #pragma unroll
         for (int p = 0; p < kRowsPages; ++p) {
-          S[p] = f32x4{0.f, 0.f, 0.f, 0.f};
+          const int t0 = b.page(min(i0 + p, b.n_pages - 1)) * kPage + 4 * grp;
+          const bool ok = (there >> p) & 1;
 #pragma unroll
-          for (int c = 0; c < NK; ++c)
-            S[p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(*(const f16x8*)(base + (p * 2 * NK + c) * 1024), q[t][c],
-                                                          S[p], 0, 0, 0);
-        }
-        if (!whole) {
-#pragma unroll
-          for (int p = 0; p < kRowsPages; ++p)
+          for (int t = 0; t < TILES; ++t)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-              const bool seen = there[p] & b.sees(number[p] * kPage + 4 * grp + v, pos[t]);
-              S[p][v] = seen ? S[p][v] : -INFINITY;  // a select, no branch
+              const bool seen = ok & b.sees(t0 + v, pos[t]);
+              S[t][p][v] = seen ? S[t][p][v] : -INFINITY;  // a select, no branch
             }
         }
+      }
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
         float mx = -INFINITY;
 #pragma unroll
         for (int p = 0; p < kRowsPages; ++p)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) mx = fmaxf(mx, S[p][v]);
-        mx = max4(fmaxf(m_run[t], mx * a.scale_log2));
-        const float alpha = __builtin_amdgcn_exp2f(m_run[t] - mx);
-        m_run[t] = mx;
+          for (int v = 0; v < 4; ++v) mx = fmaxf(mx, S[t][p][v]);
+        mx = max4(mx * a.scale_log2);
+        float alpha = 1.f;
+        if (__any(mx > m_run[t] + kRise)) {
+          const float top = mx > m_run[t] + kRise ? mx : m_run[t];
+          alpha = __builtin_amdgcn_exp2f(m_run[t] - top);
+          m_run[t] = top;
+#pragma unroll
+          for (int n = 0; n < 2 * NK; ++n) O[t][n] *= alpha;
+        }
+        mx = m_run[t];
         float l = 0.f;
 #pragma unroll
         for (int p = 0; p < kRowsPages; ++p)
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            const float e = __builtin_amdgcn_exp2f(S[p][v] * a.scale_log2 - mx);
+            const float e = __builtin_amdgcn_exp2f(S[t][p][v] * a.scale_log2 - mx);
             l += e;
             P[t][p >> 1][(p & 1) * 4 + v] = (_Float16)e;
           }
         l_run[t] = l_run[t] * alpha + l;
-        if (__any(alpha != 1.f)) {  // most steps raise no row's maximum
-#pragma unroll
-          for (int n = 0; n < 2 * NK; ++n) O[t][n] *= alpha;
-        }
       }
       // two pages per MFMA: k = 8 grp + 4 b + u is token 4 grp + u of page 2 h + b
-#pragma unroll
-      for (int h = 0; h < kRowsPages / 2; ++h) {
-        uint2 ka = {~0u, ~0u}, kb = {~0u, ~0u};
-        if (!whole) {
-          ka = keep16(b, number[2 * h] * kPage + 4 * grp, there[2 * h]);
-          kb = keep16(b, number[2 * h + 1] * kPage + 4 * grp, there[2 * h + 1]);
-        }
+      auto products = [&](int h, auto keep) {
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
-          const uint4 va = *(const uint4*)(base + (4 * h * NK + NK + i) * 1024);
-          const uint4 vb = *(const uint4*)(base + ((4 * h + 2) * NK + NK + i) * 1024);
-          const f16x8 v0 = __builtin_bit_cast(f16x8, uint4{va.x & ka.x, va.y & ka.y, vb.x & kb.x, vb.y & kb.y});
-          const f16x8 v1 = __builtin_bit_cast(f16x8, uint4{va.z & ka.x, va.w & ka.y, vb.z & kb.x, vb.w & kb.y});
+          const uint4 va = keep(*(const uint4*)(base + (4 * h * NK + NK + i) * 1024), 2 * h);
+          const uint4 vb = keep(*(const uint4*)(base + ((4 * h + 2) * NK + NK + i) * 1024), 2 * h + 1);
+          const f16x8 v0 = __builtin_bit_cast(f16x8, uint4{va.x, va.y, vb.x, vb.y});
+          const f16x8 v1 = __builtin_bit_cast(f16x8, uint4{va.z, va.w, vb.z, vb.w});
 #pragma unroll
           for (int t = 0; t < TILES; ++t) {
             O[t][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, P[t][h], O[t][2 * i], 0, 0, 0);
             O[t][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, P[t][h], O[t][2 * i + 1], 0, 0, 0);
           }
         }
+      };
+      if (clean) {
+#pragma unroll
+        for (int h = 0; h < kRowsPages / 2; ++h) products(h, [](uint4 v, int) { return v; });
+      } else {
+        uint2 k[kRowsPages];
+#pragma unroll
+        for (int p = 0; p < kRowsPages; ++p)
+          k[p] = keep16(b, b.page(min(i0 + p, b.n_pages - 1)) * kPage + 4 * grp, (there >> p) & 1);
+#pragma unroll
+        for (int h = 0; h < kRowsPages / 2; ++h)
+          products(h, [&](uint4 v, int p) { return both(v, uint4{k[p].x, k[p].y, k[p].x, k[p].y}); });
       }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();  // step st has been read: its slot may be refilled
-    asm volatile("" ::: "memory");
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // step st has been read (see the barrier)
   }
 
 #pragma unroll
