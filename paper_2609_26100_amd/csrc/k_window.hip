@@ -28,6 +28,7 @@
 
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 namespace tss {
 
@@ -109,15 +110,12 @@ __device__ __forceinline__ Block make_block(const WindowArgs& a, int s, int firs
   return b;
 }
 
-// What rows of positions a to b (at least -1) see of a walk, by places: pages
-// first .. last hold some token of their windows, of all_first .. all_last all see
-// all.  Pages of sinks come besides: the walk begins with them, so that page i
-// of the sequence is at place i.
+// Places of a walk whose pages' tokens rows of positions a to b (at least -1) all
+// have in their windows.  Pages of sinks come besides: the walk begins with them,
+// so that page i of the sequence is at place i.
 struct Span {
-  int first, last, all_first, all_last;
+  int all_first, all_last;
   __device__ Span(const Block& w, int a, int b) {
-    first = w.place(max(0, a - w.window + 1) / kPage);
-    last = b < 0 ? -1 : w.place(b / kPage);
     all_first = w.place(b - w.window < 0 ? 0 : (b - w.window) / kPage + 1);
     all_last = w.place((a + 1) / kPage - 1);
   }
@@ -405,7 +403,7 @@ __global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(WindowArgs a
   const Span span(b, wlo, whi);
   // pages that the sinks fill, and pages of whose tokens each is seen by some row
   // of the block: its first row's from the window's start, its last row's to the end
-  const int full_sinks = b.sinks / kPage, sink_end = (b.sinks + kPage - 1) / kPage;
+  const int full_sinks = b.sinks / kPage;
   const int live_first = b.place(b.lo - b.window < 0 ? 0 : (b.lo - b.window) / kPage + 1);
   const int live_last = b.place((b.hi + 1) / kPage - 1);
 
@@ -454,8 +452,9 @@ __global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(WindowArgs a
     load_ids(0);
     issue(0);
   }
-  for (int st = 0; st < n_st; ++st) {
-    const unsigned there = (unsigned)(good >> ((st * kRowsPages) & 63)) & ((1u << kRowsPages) - 1);
+  unsigned there = 0;  // bit p: page p of the step is one of the walk's and the pool's
+  auto arrive = [&](int st) {
+    there = (unsigned)(good >> ((st * kRowsPages) & 63)) & ((1u << kRowsPages) - 1);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();  // every wave's page of step st has landed, and step st - 1 has been read
     asm volatile("" ::: "memory");
@@ -463,98 +462,115 @@ __global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(WindowArgs a
       if (((st + 1) & 15) == 0) load_ids(st + 1);
       issue(st + 1);
     }
-    // some token is seen by a row of the wave; all by all of them; each by some row of the block
+  };
+  // Step st.  EDGE: some of its tokens are seen by no row of the block.
+  auto step = [&](int st, auto edge) {
+    constexpr bool EDGE = decltype(edge)::value;
+    const uint8_t* base = ring + (st % kRowsStages) * STAGE + lane * 16;
     const int i0 = (st0 + st) * kRowsPages, i1 = i0 + kRowsPages - 1;
-    const bool any = i0 <= span.last && (i0 < sink_end || i1 >= span.first);
-    const bool all_there = there == (1u << kRowsPages) - 1, in_sinks = i1 < full_sinks;
-    const bool whole = all_there && i1 <= span.all_last && (in_sinks || i0 >= span.all_first);
-    const bool clean = all_there && i1 <= live_last && (in_sinks || i0 >= live_first);
-    if (on && any) {
-      const uint8_t* base = ring + (st % kRowsStages) * STAGE + lane * 16;
-      f16x8 P[TILES][2];
-      f32x4 S[TILES][kRowsPages];
+    f16x8 P[TILES][2];
+    f32x4 S[TILES][kRowsPages];
 #pragma unroll
-      for (int p = 0; p < kRowsPages; ++p) {
+    for (int p = 0; p < kRowsPages; ++p) {
 #pragma unroll
-        for (int t = 0; t < TILES; ++t) S[t][p] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < TILES; ++t) S[t][p] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < NK; ++c) {
-          const f16x8 k = *(const f16x8*)(base + (p * 2 * NK + c) * 1024);
+      for (int c = 0; c < NK; ++c) {
+        const f16x8 k = *(const f16x8*)(base + (p * 2 * NK + c) * 1024);
 #pragma unroll
-          for (int t = 0; t < TILES; ++t) S[t][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[t][c], S[t][p], 0, 0, 0);
-        }
-      }
-      if (!whole) {
-#pragma unroll
-        for (int p = 0; p < kRowsPages; ++p) {
-          const int t0 = b.page(min(i0 + p, b.n_pages - 1)) * kPage + 4 * grp;
-          const bool ok = (there >> p) & 1;
-#pragma unroll
-          for (int t = 0; t < TILES; ++t)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              const bool seen = ok & b.sees(t0 + v, pos[t]);
-              S[t][p][v] = seen ? S[t][p][v] : -INFINITY;  // a select, no branch
-            }
-        }
-      }
-#pragma unroll
-      for (int t = 0; t < TILES; ++t) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int p = 0; p < kRowsPages; ++p)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) mx = fmaxf(mx, S[t][p][v]);
-        mx = max4(mx * a.scale_log2);
-        float alpha = 1.f;
-        if (__any(mx > m_run[t] + kRise)) {
-          const float top = mx > m_run[t] + kRise ? mx : m_run[t];
-          alpha = __builtin_amdgcn_exp2f(m_run[t] - top);
-          m_run[t] = top;
-#pragma unroll
-          for (int n = 0; n < 2 * NK; ++n) O[t][n] *= alpha;
-        }
-        mx = m_run[t];
-        float l = 0.f;
-#pragma unroll
-        for (int p = 0; p < kRowsPages; ++p)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const float e = __builtin_amdgcn_exp2f(S[t][p][v] * a.scale_log2 - mx);
-            l += e;
-            P[t][p >> 1][(p & 1) * 4 + v] = (_Float16)e;
-          }
-        l_run[t] = l_run[t] * alpha + l;
-      }
-      // two pages per MFMA: k = 8 grp + 4 b + u is token 4 grp + u of page 2 h + b
-      auto products = [&](int h, auto keep) {
-#pragma unroll
-        for (int i = 0; i < NK; ++i) {
-          const uint4 va = keep(*(const uint4*)(base + (4 * h * NK + NK + i) * 1024), 2 * h);
-          const uint4 vb = keep(*(const uint4*)(base + ((4 * h + 2) * NK + NK + i) * 1024), 2 * h + 1);
-          const f16x8 v0 = __builtin_bit_cast(f16x8, uint4{va.x, va.y, vb.x, vb.y});
-          const f16x8 v1 = __builtin_bit_cast(f16x8, uint4{va.z, va.w, vb.z, vb.w});
-#pragma unroll
-          for (int t = 0; t < TILES; ++t) {
-            O[t][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, P[t][h], O[t][2 * i], 0, 0, 0);
-            O[t][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, P[t][h], O[t][2 * i + 1], 0, 0, 0);
-          }
-        }
-      };
-      if (clean) {
-#pragma unroll
-        for (int h = 0; h < kRowsPages / 2; ++h) products(h, [](uint4 v, int) { return v; });
-      } else {
-        uint2 k[kRowsPages];
-#pragma unroll
-        for (int p = 0; p < kRowsPages; ++p)
-          k[p] = keep16(b, b.page(min(i0 + p, b.n_pages - 1)) * kPage + 4 * grp, (there >> p) & 1);
-#pragma unroll
-        for (int h = 0; h < kRowsPages / 2; ++h)
-          products(h, [&](uint4 v, int p) { return both(v, uint4{k[p].x, k[p].y, k[p].x, k[p].y}); });
+        for (int t = 0; t < TILES; ++t) S[t][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[t][c], S[t][p], 0, 0, 0);
       }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // step st has been read (see the barrier)
+    const bool whole = i1 <= span.all_last && (i1 < full_sinks || i0 >= span.all_first);
+    if (EDGE || !whole) {
+#pragma unroll
+      for (int p = 0; p < kRowsPages; ++p) {
+        const int t0 = b.page(min(i0 + p, b.n_pages - 1)) * kPage + 4 * grp;
+        const bool ok = !EDGE || ((there >> p) & 1);
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const bool seen = ok & b.sees(t0 + v, pos[t]);
+            S[t][p][v] = seen ? S[t][p][v] : -INFINITY;  // a select, no branch
+          }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int p = 0; p < kRowsPages; ++p)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) mx = fmaxf(mx, S[t][p][v]);
+      mx = max4(mx * a.scale_log2);
+      if (__any(mx > m_run[t] + kRise)) {
+        const float top = mx > m_run[t] + kRise ? mx : m_run[t];
+        const float alpha = __builtin_amdgcn_exp2f(m_run[t] - top);
+        m_run[t] = top;
+        l_run[t] *= alpha;
+#pragma unroll
+        for (int n = 0; n < 2 * NK; ++n) O[t][n] *= alpha;
+      }
+#pragma unroll
+      for (int p = 0; p < kRowsPages; ++p)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float e = __builtin_amdgcn_exp2f(S[t][p][v] * a.scale_log2 - m_run[t]);
+          l_run[t] += e;
+          P[t][p >> 1][(p & 1) * 4 + v] = (_Float16)e;
+        }
+    }
+    uint4 keep[kRowsPages];
+    if constexpr (EDGE) {
+#pragma unroll
+      for (int p = 0; p < kRowsPages; ++p) {
+        const uint2 k = keep16(b, b.page(min(i0 + p, b.n_pages - 1)) * kPage + 4 * grp, (there >> p) & 1);
+        keep[p] = uint4{k.x, k.y, k.x, k.y};
+      }
+    }
+    // two pages per MFMA: k = 8 grp + 4 b + u is token 4 grp + u of page 2 h + b
+#pragma unroll
+    for (int h = 0; h < kRowsPages / 2; ++h)
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        uint4 va = *(const uint4*)(base + (4 * h * NK + NK + i) * 1024);
+        uint4 vb = *(const uint4*)(base + ((4 * h + 2) * NK + NK + i) * 1024);
+        if constexpr (EDGE) {
+          va = both(va, keep[2 * h]);
+          vb = both(vb, keep[2 * h + 1]);
+        }
+        const f16x8 v0 = __builtin_bit_cast(f16x8, uint4{va.x, va.y, vb.x, vb.y});
+        const f16x8 v1 = __builtin_bit_cast(f16x8, uint4{va.z, va.w, vb.z, vb.w});
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+          O[t][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, P[t][h], O[t][2 * i], 0, 0, 0);
+          O[t][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, P[t][h], O[t][2 * i + 1], 0, 0, 0);
+        }
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // step st has been read (see arrive)
+  };
+  auto clean = [&](int st) {
+    const int i0 = (st0 + st) * kRowsPages, i1 = i0 + kRowsPages - 1;
+    return there == (1u << kRowsPages) - 1 && i1 <= live_last && (i1 < full_sinks || i0 >= live_first);
+  };
+  // Clean steps and those at an edge in loops of their own: in one loop the
+  // outputs' registers would be moved about between the two bodies.
+  int st = 0;
+  if (n_st > 0) arrive(0);
+  while (st < n_st) {
+    if (!on) {
+      if (++st < n_st) arrive(st);
+      continue;
+    }
+    while (st < n_st && !clean(st)) {
+      step(st, std::true_type{});
+      if (++st < n_st) arrive(st);
+    }
+    while (st < n_st && clean(st)) {
+      step(st, std::false_type{});
+      if (++st < n_st) arrive(st);
+    }
   }
 
 #pragma unroll
