@@ -672,7 +672,7 @@ Plan plan(bool f16, int n_heads, int group, int n_seqs, int max_rows, int max_le
     pages = std::min<int64_t>(pages, (sinks + kPage - 1) / kPage + (window + block_rows + 2 * kPage - 3) / kPage);
   const int64_t wgs = (int64_t)n_heads * n_seqs * p.blocks;
   const bool few = p.rows == kFewRows;
-  const int64_t target = few ? 256 : 512, least = few ? 32 : 16;
+  const int64_t target = few ? 256 : 512, least = 16;
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, target / std::max<int64_t>(1, wgs), pages / least}));
   return p;
 }
