@@ -188,6 +188,19 @@ int tss_kv_alloc(tss_ctx* ctx, int32_t n_seqs, int32_t max_tokens_per_seq, void*
  * for the whole request; the empty set for unsupported domains). */
 int tss_set_skip_mask(tss_ctx* ctx, int32_t seq, const uint8_t* mask);
 
+/* Sets the attention window of a sequence: from now on its tokens see its first
+ * `sinks` tokens and, of the others, the last `window` ones up to themselves
+ * (token t is seen from position p when t <= p and t < sinks or t > p - window).
+ * window 0, the state after tss_kv_alloc, sees all of them; otherwise it is at
+ * least 64, so that every node of a draft tree sees all of its ancestors.
+ * Attention then reads the pages of the sinks and the window instead of the
+ * whole context, in prefill, verify, batches and sweeps.  Positions and the
+ * sequence's capacity are as without a window, and tokens that are not seen stay
+ * in the cache (a wider window set later sees them again).  TSS_EINVAL for an
+ * unknown sequence, negative sinks or another window.  Paper: Problem
+ * Formulation (verification against the cached prefix, here a part of it). */
+int tss_set_window(tss_ctx* ctx, int32_t seq, int32_t sinks, int32_t window);
+
 /* Appends n context tokens to sequence seq under its skip mask: their K/V are
  * computed and kept for every layer the mask runs.  The tokens go through the
  * decoder in chunks of min(64, rows of one step); in the TSS_BF16 mode more
@@ -340,6 +353,27 @@ int tss_get_path(tss_ctx* ctx, int32_t index, int32_t* path_nodes, int32_t* path
  * TSS_EINVAL otherwise).  Paper: Problem Formulation (the committed prefix). */
 int tss_seq_length(tss_ctx* ctx, int32_t seq, int32_t* n_kv);
 int tss_seq_truncate(tss_ctx* ctx, int32_t seq, int32_t n_kv);
+
+/* Makes sequences dst[0 .. n_dst) forks of src: each gets src's first n_kv tokens
+ * (0 <= n_kv <= its length) as its context, and src's skip mask and window.  What
+ * they held before is gone.  Their pages are copied on the device, for the
+ * layers in which src holds K/V, each page read once for all of the forks, on the
+ * context's stream (without waiting; later calls are ordered behind).
+ * TSS_EINVAL for unknown, repeated or equal sequences.  Paper: Problem
+ * Formulation (several continuations of one cached prefix). */
+int tss_seq_fork(tss_ctx* ctx, int32_t src, const int32_t* dst, int32_t n_dst, int32_t n_kv);
+
+/* Log probabilities of given tokens, entropy and the top_k alternatives of the
+ * last verify's rows 0 .. n_nodes - 1 (rows in the step's node order), from its
+ * logits, to host memory; returns when they are there.  tokens: host,
+ * [n_nodes][n_tokens], NULL for n_tokens = 0; a token outside the vocabulary gives
+ * logprob NaN and rank -1.  Limits, results and their order as
+ * tss_token_logprobs has them; outputs may be NULL.  TSS_EINVAL as for
+ * tss_get_logits, TSS_ENOSPACE where the context's workspace is too small for
+ * that many alternatives.  Paper: Algorithm 1 (the downstream metric of a task
+ * whose answer is the most probable of several). */
+int tss_get_logprobs(tss_ctx* ctx, int32_t n_nodes, const int32_t* tokens, int32_t n_tokens, int32_t top_k,
+                     float* logprob, int32_t* rank, float* entropy, float* top_logprob, int32_t* top_token);
 
 /* Pure host checks, the same code the calls above run.  Paper: Problem
  * Formulation (draft trees: each node's parent precedes it; the skip set is

@@ -12,9 +12,10 @@ constexpr int kCopyThreads = 256, kCopyLoads = 4;
 constexpr int kCopySlice = kCopyThreads * kCopyLoads * 16;
 
 __global__ __launch_bounds__(kCopyThreads) void k_copy_pages(CopyArgs a) {
-  const int i0 = blockIdx.y, src = a.src[i0];
+  const int i0 = blockIdx.y, src = a.src[i0], l = blockIdx.z;
+  if (!((a.layers[l >> 6] >> (l & 63)) & 1ull)) return;
   if (i0 > 0 && a.src[i0 - 1] == src) return;  // the first copy of this source moves them all
-  uint8_t* layer = a.pages + (size_t)blockIdx.z * a.layer_bytes;
+  uint8_t* layer = a.pages + (size_t)l * a.layer_bytes;
   const size_t at = (size_t)blockIdx.x * kCopySlice + threadIdx.x * 16;
   uint4 v[kCopyLoads];
   const uint8_t* from = layer + (size_t)src * a.page_bytes + at;

@@ -39,6 +39,7 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMaxSplits = 64;
+constexpr int kLeastPages = 16;  // pages that a split has at least
 constexpr float kLowest = -3e38f;  // running maximum of a row that has seen nothing
 // A row's reference maximum is raised where the scores exceed it by this (in
 // powers of two): probabilities up to 2^8 of the largest fit fp16 as well as
@@ -65,7 +66,9 @@ struct Block {
   int r0, rows;          // first row of the sequence, its rows
   int v0, n_v;           // first virtual row of the block, how many it has (0: nothing to do)
   int p0;                // position of the sequence's first row (may be negative: more rows than tokens)
-  int lo, hi;            // positions of the block's first and last row, at least -1
+  int lo, hi;            // positions of the block's first and last row, at least -1 (a step: lowest
+                         // position of a row, last slot that one sees)
+  int n_kv;              // a step's committed context
   int sinks, window;
   int sink_pages, win_page, n_pages;  // page i of the walk: i < sink_pages ? i : win_page + i - sink_pages
   const int32_t* table;
@@ -74,41 +77,97 @@ struct Block {
   // position of a virtual row
   __device__ int pos(int v, int group) const { return max(p0 + v / group, -1); }
   __device__ bool sees(int t, int p) const { return (t <= p) & ((t < sinks) | (t > p - window)); }
-  // every row from position a to b sees all of the page, resp. none does
-  __device__ bool all_see(int page, int a, int b) const {
-    const int t = page * kPage;
-    return t + kPage - 1 <= a && (t + kPage - 1 < sinks || t > b - window);
-  }
-  __device__ bool none_sees(int page, int a, int b) const {
-    const int t = page * kPage;
-    return t > b || (t >= sinks && t + kPage - 1 <= a - window);
-  }
   // the walk's place of a page from win_page on
   __device__ int place(int page) const { return page - win_page + sink_pages; }
   // some row of the block sees the token
   __device__ bool live(int t) const { return (t <= hi) & ((t < sinks) | (t > lo - window)); }
 };
 
+// Cuts the block out of rows at positions b.p0 on and lays out its walk.
+__device__ __forceinline__ void lay_out(Block& b, int first, int most, int n_rows, int group) {
+  b.v0 = first;
+  b.n_v = max(0, min(most, n_rows * group - first));
+  if (b.n_v == 0) return;
+  b.lo = b.pos(first, group);
+  b.hi = b.pos(first + b.n_v - 1, group);
+}
+__device__ __forceinline__ void lay_walk(Block& b) {
+  if (b.n_v == 0 || b.hi < 0) return;  // no page
+  b.win_page = max(0, max(b.lo, 0) - b.window + 1) / kPage;
+  b.sink_pages = min((b.sinks + kPage - 1) / kPage, b.win_page);
+  b.n_pages = b.sink_pages + b.hi / kPage - b.win_page + 1;
+}
+
+// Block `first` .. of sequence s of a call.
 __device__ __forceinline__ Block make_block(const WindowArgs& a, int s, int first, int most) {
   Block b{};
   b.r0 = min(max(a.row_offsets[s], 0), a.rows);
   b.rows = min(max(a.row_offsets[s + 1], b.r0), a.rows) - b.r0;
   const int len = max(0, min(min(a.lengths[s], a.max_length), a.table_stride * kPage));
   b.p0 = len - b.rows;
-  b.v0 = first;
-  b.n_v = max(0, min(most, min(b.rows, a.max_rows) * a.group - first));
   b.sinks = a.sinks;
   b.window = a.window > 0 ? a.window : INT_MAX;
   b.table = a.page_table + (size_t)s * a.table_stride;
-  if (b.n_v == 0) return b;
-  b.lo = b.pos(first, a.group);
-  b.hi = b.pos(first + b.n_v - 1, a.group);
-  if (b.hi < 0) return b;  // no page
-  b.win_page = max(0, max(b.lo, 0) - b.window + 1) / kPage;
-  b.sink_pages = min((b.sinks + kPage - 1) / kPage, b.win_page);
-  b.n_pages = b.sink_pages + b.hi / kPage - b.win_page + 1;
+  lay_out(b, first, most, min(b.rows, a.max_rows), a.group);
+  lay_walk(b);
   return b;
 }
+// Of a prefill pass.
+__device__ __forceinline__ Block make_block(const WindowPassArgs& a, int, int first, int most) {
+  Block b{};
+  b.rows = a.rows;
+  b.p0 = a.max_length - a.rows;
+  b.sinks = a.sinks;
+  b.window = a.window;
+  b.table = a.page_table;
+  lay_out(b, first, most, a.rows, 1);
+  lay_walk(b);
+  return b;
+}
+// Of item s of a step: its rows sit at and behind the end of the context, and see
+// draft slots behind it.
+__device__ __forceinline__ Block make_block(const WindowStepArgs& a, int s, int first, int most) {
+  const WindowStepArgs::Item it = a.item[s];
+  Block b{};
+  b.r0 = it.row0;
+  b.rows = it.rows;
+  b.v0 = first;
+  b.n_v = max(0, min(most, it.rows - first));
+  b.n_kv = a.sp->seq_nkv[it.seg];
+  b.sinks = it.sinks;
+  b.window = it.window;
+  b.table = a.page_table + a.pt_off[it.seg];
+  b.lo = b.n_kv;
+  b.hi = b.n_kv + it.slots - 1;
+  lay_walk(b);
+  return b;
+}
+
+// What a row sees.  In a step: of the context by its position, of the draft slots
+// itself and its ancestors (a window is at least as deep as a tree).
+template <typename A>
+struct Row {
+  int pos;
+  __device__ Row() {}
+  __device__ Row(const A& a, const Block& b, int v) : pos(b.pos(v, a.group)) {}
+  __device__ bool sees(const Block& b, int t) const { return b.sees(t, pos); }
+};
+template <>
+struct Row<WindowStepArgs> {
+  int pos, node0;
+  uint64_t anc;
+  __device__ Row() {}
+  __device__ Row(const WindowStepArgs& a, const Block& b, int v) {
+    const int r = b.r0 + v;
+    pos = b.n_kv + a.sp->depth[r];
+    node0 = b.n_kv + a.sp->row_slot0[r];
+    anc = a.sp->anc[r];
+  }
+  __device__ bool sees(const Block& b, int t) const {
+    const unsigned j = (unsigned)(t - node0);
+    return ((t < b.n_kv) & b.sees(t, pos)) | ((t >= b.n_kv) & (j < 64u) & (bool)((anc >> (j & 63u)) & 1ull));
+  }
+};
 
 // Places of a walk whose pages' tokens rows of positions a to b (at least -1) all
 // have in their windows.  Pages of sinks come besides: the walk begins with them,
@@ -120,6 +179,70 @@ struct Span {
     all_last = w.place((a + 1) / kPage - 1);
   }
 };
+
+// The span of virtual rows v .. w of a block.
+__device__ __forceinline__ Span span_of(const WindowArgs& a, const Block& b, int v, int w) {
+  return Span(b, b.pos(v, a.group), b.pos(w, a.group));
+}
+__device__ __forceinline__ Span span_of(const WindowStepArgs&, const Block& b, int, int) {
+  return Span(b, b.n_kv - 1, b.n_kv + kMaxNodes - 1);
+}
+
+// 16 bytes of a virtual row's query: from dimension 32 c + 8 grp on (fp16), 16 c + 4 grp (fp32).
+template <typename T, int HD>
+__device__ __forceinline__ uint4 load_q(const WindowArgs& a, const Block& b, int v, int head, int c, int grp) {
+  const T* q = (const T*)a.q + (size_t)(b.r0 + v / a.group) * a.q_stride + (size_t)(head * a.group + v % a.group) * HD;
+  return *(const uint4*)((const uint8_t*)q + c * 64 + grp * 16);
+}
+// The verifier's queries are fp32; fp16 modes round them to the products' operands here.
+template <typename T, int HD>
+__device__ __forceinline__ uint4 load_q_f32(const WindowArgs& a, const Block& b, int v, int head, int c, int grp) {
+  const float* q = (const float*)a.q + (size_t)(b.r0 + v) * a.q_stride + (size_t)head * HD;
+  if constexpr (sizeof(T) == 4) {
+    return *(const uint4*)(q + c * 16 + grp * 4);
+  } else {
+    const float4 x = *(const float4*)(q + c * 32 + grp * 8), y = *(const float4*)(q + c * 32 + grp * 8 + 4);
+    return __builtin_bit_cast(uint4, f16x8{(_Float16)x.x, (_Float16)x.y, (_Float16)x.z, (_Float16)x.w, (_Float16)y.x,
+                                           (_Float16)y.y, (_Float16)y.z, (_Float16)y.w});
+  }
+}
+template <typename T, int HD>
+__device__ __forceinline__ uint4 load_q(const WindowPassArgs& a, const Block& b, int v, int head, int c, int grp) {
+  return load_q_f32<T, HD>(a, b, v, head, c, grp);
+}
+template <typename T, int HD>
+__device__ __forceinline__ uint4 load_q(const WindowStepArgs& a, const Block& b, int v, int head, int c, int grp) {
+  return load_q_f32<T, HD>(a, b, v, head, c, grp);
+}
+
+// Where dimension d of a row and query head is stored; dimensions d .. d + 7 (d a multiple
+// of 8, fp16) stand together.
+template <typename T, int HD>
+__device__ __forceinline__ T* out_at(const WindowArgs& a, int row, int qh, int d) {
+  return (T*)a.o + (size_t)row * a.o_stride + (size_t)qh * HD + d;
+}
+template <typename T, int HD>
+__device__ __forceinline__ T* out_at(const WindowPassArgs& a, int row, int qh, int d) {
+  return (T*)a.o + act_index<T>(row, qh * HD + d, a.n_heads * HD);
+}
+template <typename T, int HD>
+__device__ __forceinline__ T* out_at(const WindowStepArgs& a, int row, int qh, int d) {
+  return (T*)a.o + act_index<T>(row, qh * HD + d, a.n_heads * HD);
+}
+
+// The split that a launch took, for inspection.
+__device__ __forceinline__ void report(const WindowArgs&, const Block&, int, int, int, int) {}
+__device__ __forceinline__ void report(const WindowPassArgs& a, const Block& b, int, int block, int blocks, int) {
+  a.split_out[block] = 1;
+  a.split_out[kAttnMaxItems + block] = b.n_v;
+  if (block == 0) a.split_out[2 * kAttnMaxItems] = blocks;
+}
+__device__ __forceinline__ void report(const WindowStepArgs& a, const Block& b, int item, int block, int, int splits) {
+  if (block > 0) return;
+  a.split_out[item] = splits;
+  a.split_out[kAttnMaxItems + item] = b.rows;
+  if (item == 0) a.split_out[2 * kAttnMaxItems] = gridDim.y;
+}
 
 // Words of a lane's V piece (tokens 0, 1 and 2, 3 of its group) that are kept.
 __device__ __forceinline__ uint2 keep16(const Block& b, int t, bool there) {
@@ -134,12 +257,14 @@ __device__ __forceinline__ const uint8_t* page_k(const WindowArgs& a, int id, in
   return a.kv_pages + ((size_t)id * 2 * a.n_heads + head) * (kPage * HD * sizeof(T));
 }
 
-__device__ __forceinline__ size_t out_index(const WindowArgs& a, const Block& b, int v, int head, int hd) {
-  return (size_t)(b.r0 + v / a.group) * a.o_stride + (size_t)(head * a.group + v % a.group) * hd;
-}
 // slot of a virtual row's partial state
 __device__ __forceinline__ size_t part_slot(const WindowArgs& a, const Block& b, int v, int head, int split) {
   return ((size_t)split * a.rows + b.r0 + v / a.group) * (a.n_heads * a.group) + head * a.group + v % a.group;
+}
+
+// Steps of a split: an equal share, but no fewer than `least`.
+__device__ __forceinline__ int split_steps(int steps, int splits, int least) {
+  return max(least, (steps + splits - 1) / splits);
 }
 
 // --- up to 16 virtual rows ------------------------------------------------------
@@ -153,10 +278,11 @@ template <typename T, int HD>
 struct Page {
   static constexpr int N = HD * (int)sizeof(T) / 64;
   uint4 k[N], v[N];
-  int number;   // page of the sequence (scalar)
-  bool there;   // its id is one of the pool's
+  int i, number;  // place in the walk, page of the sequence (scalars)
+  bool there;     // its id is one of the pool's
 
-  __device__ __forceinline__ void load(const WindowArgs& a, int page, int id, int head, int r16, int grp) {
+  __device__ __forceinline__ void load(const WindowArgs& a, int place, int page, int id, int head, int r16, int grp) {
+    i = place;
     number = page;
     there = (unsigned)id < (unsigned)a.n_pages;
     const uint8_t* kb = page_k<T, HD>(a, there ? id : 0, head);
@@ -193,9 +319,8 @@ __device__ __forceinline__ int dim_of(int n, int v, int grp) {
 }
 
 // grid (kv head + heads * block, sequence, split)
-template <typename T, int HD>
-__global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(WindowArgs a, int splits, float* part_o,
-                                                                  float* part_ml) {
+template <typename T, int HD, typename A>
+__global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(A a, int splits, float* part_o, float* part_ml) {
   constexpr int PP = sizeof(T) == 2 ? 2 : 1;  // pages of a step
   constexpr int N = Page<T, HD>::N, NO = HD / 16;
   constexpr int LD = 64 + 4;
@@ -206,12 +331,20 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(WindowArgs a, 
   if (b.n_v == 0) return;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int r16 = lane & 15, grp = lane >> 4;
-  const int row = b.v0 + min(r16, b.n_v - 1);      // lanes past the block's rows do the last one again
-  const int pos = b.pos(row, a.group);
+  const int vrow = b.v0 + min(r16, b.n_v - 1);     // lanes past the block's rows do the last one again
+  const Row<A> row(a, b, vrow);
+  const Span span = span_of(a, b, b.v0, b.v0 + b.n_v - 1);
+  const int full_sinks = b.sinks / kPage;
 
   // this split's pages, from `from`; wave w takes steps w, w + 8, ...
-  const int steps = (b.n_pages + PP - 1) / PP, per = (steps + splits - 1) / splits;
+  const int steps = (b.n_pages + PP - 1) / PP, per = split_steps(steps, splits, kLeastPages / PP);
   const int st0 = blockIdx.z * per, n_st = min(per, steps - st0);
+  if (head == 0 && blockIdx.z == 0 && tid == 0)
+    report(a, b, blockIdx.y, blockIdx.x / a.n_heads, gridDim.x / a.n_heads, max(1, (steps + per - 1) / per));
+  if (n_st <= 0 && blockIdx.z > 0) {  // nothing left for this split
+    if (tid < b.n_v) *(float2*)(part_ml + part_slot(a, b, b.v0 + tid, head, blockIdx.z) * 2) = make_float2(kLowest, 0.f);
+    return;
+  }
   int ids = 0;
   auto walk = [&](int st, int p) { return (st0 + st) * PP + p; };  // page p of this split's step st
   auto load_ids = [&](int st) {  // of this wave's 64 / PP steps from st on
@@ -219,12 +352,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(WindowArgs a, 
     ids = b.table[b.page(min(i, b.n_pages - 1))];
   };
   uint4 q[N];
-  {
-    const T* qr = (const T*)a.q + (size_t)(b.r0 + row / a.group) * a.q_stride +
-                  (size_t)(head * a.group + row % a.group) * HD;
 #pragma unroll
-    for (int c = 0; c < N; ++c) q[c] = *(const uint4*)((const uint8_t*)qr + c * 64 + grp * 16);
-  }
+  for (int c = 0; c < N; ++c) q[c] = load_q<T, HD>(a, b, vrow, head, c, grp);
   f32x4 o[NO];
 #pragma unroll
   for (int n = 0; n < NO; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -238,7 +367,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(WindowArgs a, 
     for (int p = 0; p < PP; ++p) {
       const int i = walk(st, p);
       const int id = __builtin_amdgcn_readlane(ids, j + p);
-      pg[p].load(a, b.page(min(i, b.n_pages - 1)), i < b.n_pages ? id : -1, head, r16, grp);
+      pg[p].load(a, i, b.page(min(i, b.n_pages - 1)), i < b.n_pages ? id : -1, head, r16, grp);
     }
   };
   auto compute = [&](Page<T, HD>* pg) {
@@ -247,11 +376,11 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(WindowArgs a, 
 #pragma unroll
     for (int p = 0; p < PP; ++p) {
       S[p] = scores<T, HD>(pg[p], q);
-      if (!pg[p].there || !b.all_see(pg[p].number, b.lo, b.hi)) {
+      if (!pg[p].there || pg[p].i > span.all_last || (pg[p].i >= full_sinks && pg[p].i < span.all_first)) {
         whole = false;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const bool seen = pg[p].there & b.sees(pg[p].number * kPage + 4 * grp + v, pos);
+          const bool seen = pg[p].there & row.sees(b, pg[p].number * kPage + 4 * grp + v);
           S[p][v] = seen ? S[p][v] : -INFINITY;
         }
       }
@@ -364,7 +493,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(WindowArgs a, 
         if (h == 0 && od == 0) *(float2*)(part_ml + slot * 2) = make_float2(top, L);
       } else {
         const float inv = L > 0.f ? 1.f / L : L;  // 0 for a row that sees nothing, NaN stays
-        T* to = (T*)a.o + out_index(a, b, v, head, HD) + 64 * h + od;
+        T* to = out_at<T, HD>(a, b.r0 + v / a.group, head * a.group + v % a.group, 64 * h + od);
         to[0] = (T)(x * inv);
         to[1] = (T)(y * inv);
       }
@@ -381,9 +510,9 @@ constexpr int kRowsWaves = 4, kRowsPages = 4, kRowsStages = 2;
 // K chunk c covers dims 32 c .. + 31 (16 tokens x 64 bytes of a page), V chunk i
 // dims 32 i .. + 31 of four token groups (4 x 256 bytes): each is one KiB load, read
 // back lane by lane in order.  grid as k_window_few.
-template <int HD, int TILES>
-__global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(WindowArgs a, int splits, int blocks,
-                                                                    float* part_o, float* part_ml) {
+template <int HD, int TILES, typename A>
+__global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(A a, int splits, int blocks, float* part_o,
+                                                                    float* part_ml) {
   constexpr int NK = HD / 32;              // KiB of a K (or V) page block
   constexpr int PW = 2 * NK;               // loads of one wave per step: one page
   constexpr int STAGE = kRowsPages * 2 * NK * 1024;
@@ -391,16 +520,24 @@ __global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(WindowArgs a
   __shared__ __align__(16) uint8_t ring[kRowsStages * STAGE];
   const int head = blockIdx.x % a.n_heads;
   // the last rows first: without a window theirs is the longest walk
-  const Block b = make_block(a, blockIdx.y, (blocks - 1 - (int)blockIdx.x / a.n_heads) * ROWS, ROWS);
+  const int block = blocks - 1 - (int)blockIdx.x / a.n_heads;
+  const Block b = make_block(a, blockIdx.y, block * ROWS, ROWS);
   if (b.n_v == 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int r16 = lane & 15, grp = lane >> 4;
-  const int steps = (b.n_pages + kRowsPages - 1) / kRowsPages, per = (steps + splits - 1) / splits;
+  const int steps = (b.n_pages + kRowsPages - 1) / kRowsPages;
+  const int per = split_steps(steps, splits, kLeastPages / kRowsPages);
   const int st0 = blockIdx.z * per, n_st = max(0, min(per, steps - st0));
+  if (head == 0 && blockIdx.z == 0 && threadIdx.x == 0)
+    report(a, b, blockIdx.y, block, blocks, max(1, (steps + per - 1) / per));
+  if (n_st == 0 && blockIdx.z > 0) {  // nothing left for this split
+    for (int i = threadIdx.x; i < b.n_v; i += kRowsWaves * 64)
+      *(float2*)(part_ml + part_slot(a, b, b.v0 + i, head, blockIdx.z) * 2) = make_float2(kLowest, 0.f);
+    return;
+  }
   const int w0 = wave * TILES * 16;                         // the wave's first row of the block
   const bool on = w0 < b.n_v;
-  const int wlo = b.pos(b.v0 + w0, a.group), whi = b.pos(b.v0 + min(w0 + TILES * 16, b.n_v) - 1, a.group);
-  const Span span(b, wlo, whi);
+  const Span span = span_of(a, b, b.v0 + w0, b.v0 + min(w0 + TILES * 16, b.n_v) - 1);
   // pages that the sinks fill, and pages of whose tokens each is seen by some row
   // of the block: its first row's from the window's start, its last row's to the end
   const int full_sinks = b.sinks / kPage;
@@ -431,17 +568,15 @@ __global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(WindowArgs a
   };
 
   f16x8 q[TILES][NK];
-  int pos[TILES];
+  Row<A> row[TILES];
   f32x4 O[TILES][2 * NK];  // [2 i + j]: dims 32 i + 8 grp + 2 v + j
   float m_run[TILES], l_run[TILES];
 #pragma unroll
   for (int t = 0; t < TILES; ++t) {
     const int v = b.v0 + min(w0 + t * 16 + r16, b.n_v - 1);
-    pos[t] = b.pos(v, a.group);
-    const _Float16* qr = (const _Float16*)a.q + (size_t)(b.r0 + v / a.group) * a.q_stride +
-                         (size_t)(head * a.group + v % a.group) * HD + grp * 8;
+    row[t] = Row<A>(a, b, v);
 #pragma unroll
-    for (int c = 0; c < NK; ++c) q[t][c] = *(const f16x8*)(qr + c * 32);
+    for (int c = 0; c < NK; ++c) q[t][c] = __builtin_bit_cast(f16x8, load_q<_Float16, HD>(a, b, v, head, c, grp));
     m_run[t] = kLowest;
     l_run[t] = 0.f;
 #pragma unroll
@@ -491,7 +626,7 @@ __global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(WindowArgs a
         for (int t = 0; t < TILES; ++t)
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            const bool seen = ok & b.sees(t0 + v, pos[t]);
+            const bool seen = ok & row[t].sees(b, t0 + v);
             S[t][p][v] = seen ? S[t][p][v] : -INFINITY;  // a select, no branch
           }
       }
@@ -591,7 +726,6 @@ __global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(WindowArgs a
       continue;
     }
     const float inv = l > 0.f ? 1.f / l : l;
-    _Float16* to = (_Float16*)a.o + out_index(a, b, v, head, HD) + 8 * grp;
 #pragma unroll
     for (int n = 0; n < NK; ++n) {
       f16x8 x;
@@ -600,23 +734,30 @@ __global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(WindowArgs a
         x[2 * u] = (_Float16)(O[t][2 * n][u] * inv);
         x[2 * u + 1] = (_Float16)(O[t][2 * n + 1][u] * inv);
       }
-      *(f16x8*)(to + 32 * n) = x;
+      *(f16x8*)out_at<_Float16, HD>(a, b.r0 + v / a.group, head * a.group + v % a.group, 32 * n + 8 * grp) = x;
     }
   }
 }
 
+// Row i of sequence (item) s, -1 for none.
+__device__ __forceinline__ int join_row(const WindowArgs& a, int s, int i) {
+  const int r0 = min(max(a.row_offsets[s], 0), a.rows), r1 = min(max(a.row_offsets[s + 1], r0), a.rows);
+  return i < r1 - r0 ? r0 + i : -1;
+}
+__device__ __forceinline__ int join_row(const WindowStepArgs& a, int s, int i) {
+  return i < a.item[s].rows ? a.item[s].row0 + i : -1;
+}
+
 // Joins the splits' states, a workgroup for each (row, query head), a quarter of
 // the splits for each of its waves.  grid (rows of a sequence, sequence, query head).
-template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_window_join(WindowArgs a, int splits, const float* part_o,
-                                                     const float* part_ml) {
+template <typename T, int HD, typename A>
+__global__ __launch_bounds__(256) void k_window_join(A a, int splits, const float* part_o, const float* part_ml) {
   constexpr int N = HD / 64;
   __shared__ float s_o[4][HD];
   const int s = blockIdx.y, qh = blockIdx.z, heads = a.n_heads * a.group;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int r0 = min(max(a.row_offsets[s], 0), a.rows), r1 = min(max(a.row_offsets[s + 1], r0), a.rows);
-  const int row = r0 + blockIdx.x;
-  if (row >= r1) return;
+  const int row = join_row(a, s, blockIdx.x);
+  if (row < 0) return;
   const size_t slot = (size_t)row * heads + qh, stride = (size_t)a.rows * heads;
   float2 ml = make_float2(kLowest, 0.f);
   if (lane < splits) ml = *(const float2*)(part_ml + (slot + lane * stride) * 2);
@@ -642,7 +783,7 @@ __global__ __launch_bounds__(256) void k_window_join(WindowArgs a, int splits, c
     if (g >= splits) break;
     const float w = __shfl(f, g);
 #pragma unroll
-    for (int n = 0; n < N; ++n) o[n] += w * p[i][n];
+    for (int n = 0; n < N; ++n) o[n] += w == 0.f ? 0.f : w * p[i][n];  // a split without pages has written no output
   }
 #pragma unroll
   for (int n = 0; n < N; ++n) s_o[wave][lane * N + n] = o[n];
@@ -650,31 +791,36 @@ __global__ __launch_bounds__(256) void k_window_join(WindowArgs a, int splits, c
   if (threadIdx.x < HD) {
     const int d = threadIdx.x;
     const float x = (s_o[0][d] + s_o[1][d]) + (s_o[2][d] + s_o[3][d]);
-    ((T*)a.o)[(size_t)row * a.o_stride + (size_t)qh * HD + d] = (T)(x * (L > 0.f ? 1.f / L : L));
+    *out_at<T, HD>(a, row, qh, d) = (T)(x * (L > 0.f ? 1.f / L : L));
   }
 }
 
-// How a call is cut up: virtual rows of a block, blocks of a sequence, splits of
-// a block's pages.  Splits are worth their second launch where the
-// blocks leave most of the chip idle and each still has some pages to walk.
+// How a launch is cut up: virtual rows of a block, blocks of a sequence, splits of
+// a block's pages.  Splits are worth their second launch where the blocks leave
+// most of the chip idle and each still has some pages to walk: one row over 1028
+// tokens of 32 heads 15.1 us in one split, 10.8 + 3.6 in two, 8.4 + 3.0 in four.
 struct Plan {
   int rows, blocks, splits;
 };
-Plan plan(bool f16, int n_heads, int group, int n_seqs, int max_rows, int max_length, int sinks, int window) {
-  const int64_t v = (int64_t)max_rows * group;
+// pages: most that a walk can have; seqs: sequences or items.
+Plan plan(bool f16, int n_heads, int64_t v_rows, int64_t seqs, int64_t pages) {
   Plan p;
-  p.rows = !f16 || v <= kFewRows ? kFewRows : v <= kRowsWaves * 16 ? kRowsWaves * 16 : kRowsWaves * 32;
-  p.blocks = (int)((v + p.rows - 1) / p.rows);
-  // pages of the longest walk
-  const int64_t block_rows = std::min<int64_t>(max_rows, (p.rows + group - 1) / group + 1);
-  int64_t pages = (max_length + kPage - 1) / kPage;
-  if (window > 0)
-    pages = std::min<int64_t>(pages, (sinks + kPage - 1) / kPage + (window + block_rows + 2 * kPage - 3) / kPage);
-  const int64_t wgs = (int64_t)n_heads * n_seqs * p.blocks;
-  const bool few = p.rows == kFewRows;
-  const int64_t target = few ? 256 : 512, least = 16;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, target / std::max<int64_t>(1, wgs), pages / least}));
+  p.rows = !f16 || v_rows <= kFewRows ? kFewRows : v_rows <= kRowsWaves * 16 ? kRowsWaves * 16 : kRowsWaves * 32;
+  p.blocks = (int)((v_rows + p.rows - 1) / p.rows);
+  // a wave of few rows takes most of a SIMD's registers: one workgroup a CU
+  const int64_t target = p.rows == kFewRows ? 256 : 512, wgs = n_heads * seqs * p.blocks;
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, target / wgs, pages / kLeastPages}));
   return p;
+}
+// Pages that a block of `rows` rows walks at most.
+int64_t walk_pages(int64_t rows, int64_t max_length, int64_t sinks, int64_t window) {
+  const int64_t all = (max_length + kPage - 1) / kPage;
+  return window > 0 ? std::min(all, (sinks + kPage - 1) / kPage + (window + rows + 2 * kPage - 3) / kPage) : all;
+}
+Plan plan(bool f16, int n_heads, int group, int n_seqs, int max_rows, int max_length, int sinks, int window) {
+  Plan p = plan(f16, n_heads, (int64_t)max_rows * group, n_seqs, INT_MAX);
+  const int64_t rows = std::min<int64_t>(max_rows, (p.rows + group - 1) / group + 1);
+  return plan(f16, n_heads, (int64_t)max_rows * group, n_seqs, walk_pages(rows, max_length, sinks, window));
 }
 
 }  // namespace
@@ -698,16 +844,16 @@ static hipError_t launch_typed(const WindowArgs& a, float* ws, hipStream_t s) {
   float* part_ml = ws + (size_t)p.splits * a.rows * a.n_heads * a.group * HD;
   const dim3 grid(a.n_heads * p.blocks, a.n_seqs, p.splits);
   if (p.rows == kFewRows) {
-    TSS_LAUNCH((k_window_few<T, HD>), grid, dim3(kFewWaves * 64), 0, s, a, p.splits, part_o, part_ml);
+    TSS_LAUNCH((k_window_few<T, HD, WindowArgs>), grid, dim3(kFewWaves * 64), 0, s, a, p.splits, part_o, part_ml);
   } else if constexpr (sizeof(T) == 2) {
     if (p.rows == kRowsWaves * 16)
-      TSS_LAUNCH((k_window_rows<HD, 1>), grid, dim3(kRowsWaves * 64), 0, s, a, p.splits, p.blocks, part_o, part_ml);
+      TSS_LAUNCH((k_window_rows<HD, 1, WindowArgs>), grid, dim3(kRowsWaves * 64), 0, s, a, p.splits, p.blocks, part_o, part_ml);
     else
-      TSS_LAUNCH((k_window_rows<HD, 2>), grid, dim3(kRowsWaves * 64), 0, s, a, p.splits, p.blocks, part_o, part_ml);
+      TSS_LAUNCH((k_window_rows<HD, 2, WindowArgs>), grid, dim3(kRowsWaves * 64), 0, s, a, p.splits, p.blocks, part_o, part_ml);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  TSS_LAUNCH((k_window_join<T, HD>), dim3(a.max_rows, a.n_seqs, a.n_heads * a.group), dim3(256), 0, s, a,
+  TSS_LAUNCH((k_window_join<T, HD, WindowArgs>), dim3(a.max_rows, a.n_seqs, a.n_heads * a.group), dim3(256), 0, s, a,
              p.splits, part_o, part_ml);
   return hipGetLastError();
 }
@@ -716,6 +862,59 @@ hipError_t launch_window(bool f16, int head_dim, const WindowArgs& a, void* work
   float* ws = (float*)workspace;
   if (f16) return head_dim == 128 ? launch_typed<_Float16, 128>(a, ws, s) : launch_typed<_Float16, 64>(a, ws, s);
   return head_dim == 128 ? launch_typed<float, 128>(a, ws, s) : launch_typed<float, 64>(a, ws, s);
+}
+
+hipError_t launch_window_pass(int head_dim, const WindowPassArgs& a, hipStream_t s) {
+  if (a.rows < 1 || a.rows > kPromptRows) return hipErrorInvalidValue;
+  const int blocks = (a.rows + kRowsWaves * 32 - 1) / (kRowsWaves * 32);  // passes take more than 64 rows
+  const dim3 grid(a.n_heads * blocks, 1, 1), block(kRowsWaves * 64);
+  float* none = nullptr;
+  if (head_dim == 128)
+    TSS_LAUNCH((k_window_rows<128, 2, WindowPassArgs>), grid, block, 0, s, a, 1, blocks, none, none);
+  else
+    TSS_LAUNCH((k_window_rows<64, 2, WindowPassArgs>), grid, block, 0, s, a, 1, blocks, none, none);
+  return hipGetLastError();
+}
+
+template <typename T, int HD>
+static hipError_t launch_step_typed(int n_items, const WindowStepArgs& a, float* part_o, float* part_ml,
+                                    size_t part_slots, hipStream_t s) {
+  int64_t rows = 0, pages = 0;
+  for (int i = 0; i < n_items; ++i) {
+    const WindowStepArgs::Item& it = a.item[i];
+    rows = std::max<int64_t>(rows, it.rows);
+    // rows at the context's end and draft slots behind it
+    pages = std::max(pages, walk_pages(it.slots, a.max_length, it.sinks, it.window == INT_MAX ? 0 : it.window));
+  }
+  Plan p = plan(sizeof(T) == 2, a.n_heads, rows, n_items, pages);
+  if (p.rows > kRowsWaves * 16) return hipErrorInvalidValue;  // items have at most 64 rows
+  // a slot holds 64 rows of one head
+  p.splits = (int)std::min<int64_t>(p.splits, std::max<int64_t>(1, part_slots * 64 / ((int64_t)a.rows * a.n_heads)));
+  const dim3 grid(a.n_heads * p.blocks, n_items, p.splits);
+  if (p.rows == kFewRows)
+    TSS_LAUNCH((k_window_few<T, HD, WindowStepArgs>), grid, dim3(kFewWaves * 64), 0, s, a, p.splits, part_o, part_ml);
+  else if constexpr (sizeof(T) == 2)
+    TSS_LAUNCH((k_window_rows<HD, 1, WindowStepArgs>), grid, dim3(kRowsWaves * 64), 0, s, a, p.splits, p.blocks, part_o,
+               part_ml);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  // the timing of a launch is that of the one above
+  const LaunchTiming timing = launch_timing();
+  launch_timing() = LaunchTiming{};
+  TSS_LAUNCH((k_window_join<T, HD, WindowStepArgs>), dim3(rows, n_items, a.n_heads), dim3(256), 0, s, a, p.splits, part_o,
+             part_ml);
+  launch_timing() = timing;
+  return hipGetLastError();
+}
+
+hipError_t launch_window_step(bool f16, int head_dim, int n_items, const WindowStepArgs& a, float* part_o,
+                              float* part_ml, size_t part_slots, hipStream_t s) {
+  if (n_items < 1 || n_items > kAttnMaxItems) return hipErrorInvalidValue;
+  if (f16)
+    return head_dim == 128 ? launch_step_typed<_Float16, 128>(n_items, a, part_o, part_ml, part_slots, s)
+                           : launch_step_typed<_Float16, 64>(n_items, a, part_o, part_ml, part_slots, s);
+  return head_dim == 128 ? launch_step_typed<float, 128>(n_items, a, part_o, part_ml, part_slots, s)
+                         : launch_step_typed<float, 64>(n_items, a, part_o, part_ml, part_slots, s);
 }
 
 }  // namespace tss

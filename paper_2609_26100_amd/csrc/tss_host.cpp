@@ -46,6 +46,7 @@ struct WeightLayout {
 struct WsLayout {
   size_t sp, rows, result, h, xa, xm, ss_a, ss_m, q, o, act, part_o, part_ml, counters, attn_split, kpart, kcount, acount, logits,
       am_val, am_idx, greedy, kpart_bytes, total;
+  size_t part_slots;  // of part_o and part_ml, 64 rows of one head each
   int n_counters;
 };
 
@@ -204,6 +205,8 @@ WsLayout ws_layout(const tss_model_cfg* c) {
   w.o = take(ap * Mp * d * es);
   w.act = take(ap * Mp * f * es);
   const size_t slots = attn_slots(c);
+  static_assert(kAttnMaxTiles * 16 == 64, "rows of a slot");
+  w.part_slots = slots;
   w.part_o = take(slots * kAttnMaxTiles * 16 * c->head_dim * 4);
   w.part_ml = take(slots * kAttnMaxTiles * 16 * 2 * 4);
   // arrival counters of the attention merges, of the K-split strips and of
@@ -292,6 +295,12 @@ struct tss_ctx {
   std::vector<int32_t> pt_host;   // host copy of the page tables
   std::vector<std::vector<int32_t>> kv_len;
   std::vector<std::vector<uint8_t>> mask;
+  // attention window of each sequence: it sees its first `sinks` tokens and its last
+  // `window` ones (0: all)
+  struct Window {
+    int32_t sinks = 0, window = 0;
+  };
+  std::vector<Window> window;
   // pinned host staging: step parameters and result, and two weight-upload
   // buffers (packing one while the other is copied)
   uint8_t* stage[2] = {nullptr, nullptr};
@@ -732,6 +741,7 @@ int tss_kv_alloc(tss_ctx* c, int32_t n_seqs, int32_t max_tokens_per_seq, void* d
   c->n_kv.assign(n_seqs, 0);
   c->kv_len.assign(n_seqs, std::vector<int32_t>(c->cfg.n_layers, 0));
   c->mask.assign(n_seqs, std::vector<uint8_t>(c->cfg.n_layers, 0));
+  c->window.assign(n_seqs, tss_ctx::Window{});
   return TSS_OK;
 }
 
@@ -740,6 +750,17 @@ int tss_set_skip_mask(tss_ctx* c, int32_t seq, const uint8_t* mask) {
   if (seq < 0 || seq >= c->n_seqs) return fail(c, TSS_EINVAL, "unknown sequence");
   if (mask && !mask_ok(mask, c->cfg.n_layers)) return fail(c, TSS_EINVAL, "mask bytes must be 0 or 1");
   for (int l = 0; l < c->cfg.n_layers; ++l) c->mask[seq][l] = mask ? mask[l] : 0;
+  return TSS_OK;
+}
+
+int tss_set_window(tss_ctx* c, int32_t seq, int32_t sinks, int32_t window) {
+  if (!c) return TSS_EINVAL;
+  if (seq < 0 || seq >= c->n_seqs) return fail(c, TSS_EINVAL, "unknown sequence");
+  if (sinks < 0 || window < 0 || (window > 0 && window < kMaxNodes))
+    return fail(c, TSS_EINVAL, "sinks must not be negative and window 0 or at least 64");
+  c->window[seq] = tss_ctx::Window{std::min(sinks, c->max_tokens), std::min(window, c->max_tokens)};
+  // a window as long as the capacity hides nothing
+  if (window >= c->max_tokens) c->window[seq] = tss_ctx::Window{};
   return TSS_OK;
 }
 
@@ -858,10 +879,11 @@ int enqueue_step(tss_ctx* c, bool verify, hipStream_t s, int start_layer = 0, co
   c->prof_armed = false;
 
   int32_t pt_off[kMaxSegs] = {};
-  bool one_seq = true;
+  bool one_seq = true, windowed = false;
   for (int i = 0; i < B; ++i) {
     pt_off[i] = st.seq[i] * pps;
     one_seq = one_seq && st.seq[i] == st.seq[0];
+    windowed = windowed || c->window[st.seq[i]].window > 0;
   }
   // with one KV sequence in the step its first page ids travel in the kernel arguments
   int32_t arg_pages[kArgPages] = {};
@@ -969,7 +991,34 @@ int enqueue_step(tss_ctx* c, bool verify, hipStream_t s, int start_layer = 0, co
       HIPCHK(project(EPI_QKV, a), "qkv gemm");
       ps.done();
     }
-    {  // tree attention
+    if (windowed) {  // attention where some sequence has a window: as below, by k_window's kernels
+      WindowStepArgs a{};
+      a.q = ws + c->wsl.q;
+      a.o = ws + c->wsl.o;
+      a.q_stride = d;
+      a.kv_pages = pages + (size_t)l * c->kvl.n_pages * 2 * H * kPage * hd * c->es;
+      a.page_table = pt_all;
+      a.n_pages = c->kvl.n_pages;
+      a.n_heads = H;
+      a.group = 1;
+      a.rows = M;
+      a.max_length = c->max_tokens;
+      a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)hd));
+      a.split_out = (int32_t*)(ws + c->wsl.attn_split);
+      a.sp = sp_dev;
+      for (int i = 0; i < n_act; ++i) {
+        const tss_ctx::Window& w = c->window[st.seq[at.item[i].seg]];
+        a.item[i] = {at.item[i].row0, at.item[i].rows, at.item[i].seg, at.item[i].slots, w.sinks,
+                     w.window > 0 ? w.window : INT32_MAX};
+      }
+      std::memcpy(a.pt_off, pt_off, sizeof(pt_off));
+      if (!launch_window_step) return fail(c, TSS_EINVAL, "built without the operators' kernels");
+      ProfScope ps(c, TSS_K_ATTN, l);
+      HIPCHK(launch_window_step(c->bf16, hd, n_act, a, (float*)(ws + c->wsl.part_o), (float*)(ws + c->wsl.part_ml),
+                                c->wsl.part_slots, s),
+             "windowed attention");
+      ps.done();
+    } else {  // tree attention
       AttnArgs& a = at;
       a.q = (const float*)(ws + c->wsl.q);
       a.kv_pages = pages;
@@ -1187,7 +1236,27 @@ int enqueue_prompt(tss_ctx* c, int seq, const int32_t* tokens, int M, int pos0) 
       ps.done();
     }
     if (l == last) break;
-    {
+    if (c->window[seq].window > 0) {
+      WindowPassArgs a{};
+      a.q = c->kv + kl.p_q;
+      a.o = c->kv + kl.p_o;
+      a.q_stride = d;
+      a.kv_pages = c->kv + kl.pages + (size_t)l * kl.n_pages * 2 * H * kPage * hd * c->es;
+      a.page_table = pt;
+      a.n_pages = kl.n_pages;
+      a.n_heads = H;
+      a.group = 1;
+      a.rows = M;
+      a.max_length = pos0 + M;
+      a.sinks = c->window[seq].sinks;
+      a.window = c->window[seq].window;
+      a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)hd));
+      a.split_out = (int32_t*)(c->ws + c->wsl.attn_split);
+      if (!launch_window_pass) return fail(c, TSS_EINVAL, "built without the operators' kernels");
+      ProfScope ps(c, TSS_K_ATTN, l);
+      HIPCHK(launch_window_pass(hd, a, s), "windowed prompt attention");
+      ps.done();
+    } else {
       PromptAttnArgs a{};
       a.q = (const float*)(c->kv + kl.p_q);
       a.kv_pages = c->kv + kl.pages;
@@ -1312,6 +1381,8 @@ int run_verify_graph(tss_ctx* c) {
     put(st.seq[i]);
     put(sp.seq_row0[i + 1] - sp.seq_row0[i]);
     put(st.compact[i]);
+    put(c->window[st.seq[i]].sinks);
+    put(c->window[st.seq[i]].window);
   }
   key.append((const char*)st.mask.data(), st.mask.size());
   tss_ctx::GraphEntry* g = nullptr;
@@ -1783,6 +1854,104 @@ int tss_check_kv(tss_ctx* c) {
       if (c->kv_len[s][l] < 0 || c->kv_len[s][l] > c->n_kv[s])
         return fail(c, TSS_ESTATE, "sequence " + std::to_string(s) + " holds K/V past its length");
   }
+  return TSS_OK;
+}
+
+int tss_seq_fork(tss_ctx* c, int32_t src, const int32_t* dst, int32_t n_dst, int32_t n_kv) {
+  if (!c) return TSS_EINVAL;
+  const int r = check_ready(c, src);
+  if (r) return r;
+  if (n_dst < 1 || !dst) return fail(c, TSS_EINVAL, "no sequence to fork to");
+  if (n_kv < 0 || n_kv > c->n_kv[src]) return fail(c, TSS_EINVAL, "a fork has at most the source's tokens");
+  for (int i = 0; i < n_dst; ++i) {
+    if (dst[i] < 0 || dst[i] >= c->n_seqs || dst[i] == src) return fail(c, TSS_EINVAL, "unknown sequence, or the source");
+    for (int j = 0; j < i; ++j)
+      if (dst[j] == dst[i]) return fail(c, TSS_EINVAL, "a sequence appears twice");
+  }
+  const tss_model_cfg& cf = c->cfg;
+  CopyArgs a{};
+  a.pages = c->kv + c->kvl.pages;
+  a.page_bytes = (size_t)2 * cf.n_heads * kPage * cf.head_dim * c->es;
+  a.layer_bytes = a.page_bytes * c->kvl.n_pages;
+  a.n_layers = cf.n_layers;
+  bool any = false;
+  for (int l = 0; l < cf.n_layers; ++l)  // layers without K/V have nothing to copy
+    if (c->kv_len[src][l] > 0) {
+      a.layers[l >> 6] |= 1ull << (l & 63);
+      any = true;
+    }
+  const int pps = c->kvl.pages_per_seq, n_pages = any ? (n_kv + kPage - 1) / kPage : 0;
+  if (n_pages > 0 && !launch_copy_pages) return fail(c, TSS_EINVAL, "built without the operators' kernels");
+  // page by page, its copies next to each other
+  for (int p = 0; p < n_pages; ++p)
+    for (int i = 0; i < n_dst; ++i) {
+      a.src[a.n] = c->pt_host[(size_t)src * pps + p];
+      a.dst[a.n] = c->pt_host[(size_t)dst[i] * pps + p];
+      if (++a.n == kCopyPairs || (p == n_pages - 1 && i == n_dst - 1)) {
+        HIPCHK(launch_copy_pages(a, c->stream), "page copies");
+        a.n = 0;
+      }
+    }
+  for (int i = 0; i < n_dst; ++i) {
+    c->n_kv[dst[i]] = n_kv;
+    for (int l = 0; l < cf.n_layers; ++l) c->kv_len[dst[i]][l] = std::min(c->kv_len[src][l], n_kv);
+    c->mask[dst[i]] = c->mask[src];
+    c->window[dst[i]] = c->window[src];
+  }
+  return TSS_OK;
+}
+
+int tss_get_logprobs(tss_ctx* c, int32_t n_nodes, const int32_t* tokens, int32_t n_tokens, int32_t top_k,
+                     float* logprob, int32_t* rank, float* entropy, float* top_logprob, int32_t* top_token) {
+  if (!c) return TSS_EINVAL;
+  if (c->poisoned) return fail(c, TSS_ESTATE, "context poisoned by an earlier HIP error");
+  if (n_nodes < 1 || n_nodes > c->last_M) return fail(c, TSS_EINVAL, "n_nodes exceeds the last verify's nodes");
+  const int V = c->cfg.vocab;
+  if (n_tokens < 0 || n_tokens > TSS_LOGPROBS_MAX_TOKENS || (n_tokens > 0 && !tokens) || top_k < 0 ||
+      top_k > TSS_LOGPROBS_MAX_TOP || top_k > V)
+    return fail(c, TSS_EINVAL, "n_tokens outside [0, 8], top_k outside [0, min(32, vocab)] or no tokens");
+  if (!launch_logprobs || !logprobs_fit(n_nodes, V)) return fail(c, TSS_EINVAL, "vocabulary too large");
+  // scratch: the attention's partial outputs, which nothing needs after the step:
+  // the given tokens, the results one behind the other, the call's own workspace
+  const size_t nt = (size_t)n_nodes * n_tokens, nk = (size_t)n_nodes * top_k;
+  const size_t words = nt + 2 * nt + n_nodes + 2 * nk;
+  const size_t own = align256(words * 4), need = own + logprobs_bytes(n_nodes, V, n_tokens, top_k);
+  if (need > c->out_wsl.part_slots * 64 * c->cfg.head_dim * 4)
+    return fail(c, TSS_ENOSPACE, "the workspace has no room for that many alternatives");
+  uint8_t* base = const_cast<uint8_t*>(c->out_ws) + c->out_wsl.part_o;
+  int32_t* dtok = (int32_t*)base;
+  LogprobArgs a{};
+  a.x = c->out_ws + c->out_wsl.logits;
+  a.stride = V;
+  a.rows = n_nodes;
+  a.vocab = V;
+  a.type = TSS_T_F32;
+  a.tokens = dtok;
+  a.n_tokens = n_tokens;
+  a.top_k = top_k;
+  a.logprob = (float*)(dtok + nt);
+  a.rank = (int32_t*)(a.logprob + nt);
+  a.entropy = (float*)(a.rank + nt);
+  a.top_logprob = a.entropy + n_nodes;
+  a.top_token = (int32_t*)(a.top_logprob + nk);
+  std::vector<int32_t> host;
+  try {
+    host.resize(words);
+  } catch (...) {
+    return fail(c, TSS_ENOSPACE, "no host memory");
+  }
+  if (nt) HIPCHK(hipMemcpyAsync(dtok, tokens, nt * 4, hipMemcpyHostToDevice, c->stream), "given tokens");
+  HIPCHK(launch_logprobs(a, base + own, c->stream), "log probabilities");
+  HIPCHK(hipMemcpyAsync(host.data() + nt, dtok + nt, (words - nt) * 4, hipMemcpyDeviceToHost, c->stream), "results");
+  HIPCHK(hipStreamSynchronize(c->stream), "log probabilities");
+  auto give = [&](void* to, const void* from_dev, size_t n) {
+    if (to && n) std::memcpy(to, host.data() + ((const int32_t*)from_dev - dtok), n * 4);
+  };
+  give(logprob, a.logprob, nt);
+  give(rank, a.rank, nt);
+  give(entropy, a.entropy, n_nodes);
+  give(top_logprob, a.top_logprob, nk);
+  give(top_token, a.top_token, nk);
   return TSS_OK;
 }
 

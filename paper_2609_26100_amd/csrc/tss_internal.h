@@ -436,9 +436,9 @@ struct LogprobArgs {
 };
 // Limits of a call: logprobs_fit is whether its workgroups can be launched.
 constexpr int kLogprobVocab = 1 << 20;
-bool logprobs_fit(int rows, int vocab);
-size_t logprobs_bytes(int rows, int vocab, int n_tokens, int top_k);
-hipError_t launch_logprobs(const LogprobArgs& a, void* workspace, hipStream_t s);
+__attribute__((weak)) bool logprobs_fit(int rows, int vocab);
+__attribute__((weak)) size_t logprobs_bytes(int rows, int vocab, int n_tokens, int top_k);
+__attribute__((weak)) hipError_t launch_logprobs(const LogprobArgs& a, void* workspace, hipStream_t s);
 
 struct WindowArgs {
   const void* q;           // [rows][n_q_heads][hd], rows q_stride elements apart
@@ -459,14 +459,39 @@ size_t window_bytes(bool f16, int head_dim, int n_heads, int group, int n_seqs, 
                     int sinks, int window);
 hipError_t launch_window(bool f16, int head_dim, const WindowArgs& a, void* workspace, hipStream_t s);
 
+// The same for the verifier's own launches where a sequence has a window: a
+// prefill pass (one sequence; rows, max_length and the page table are its own) and a
+// step (items as AttnArgs has them).  q is fp32 [rows][n_heads * hd], o the attention
+// output in act_index order.
+struct WindowPassArgs : WindowArgs {
+  int32_t* split_out;      // as AttnArgs::split_out
+};
+struct WindowStepArgs : WindowArgs {
+  int32_t* split_out;
+  const StepParams* sp;
+  struct Item {
+    int32_t row0, rows, seg, slots;  // as AttnArgs::Item
+    int32_t sinks, window;           // of its sequence; window INT32_MAX: none
+  } item[kAttnMaxItems];
+  int32_t pt_off[kMaxSegs];
+};
+// part: scratch of part_slots * 64 * (hd + 2) floats, as the attention of a step has it.
+// Weak, as the calls below: the host runtime also links without the operators'
+// kernels (its sanitizer build); a call that needs one is then refused.
+#define TSS_WEAK __attribute__((weak))
+TSS_WEAK hipError_t launch_window_pass(int head_dim, const WindowPassArgs& a, hipStream_t s);
+TSS_WEAK hipError_t launch_window_step(bool f16, int head_dim, int n_items, const WindowStepArgs& a, float* part_o,
+                                       float* part_ml, size_t part_slots, hipStream_t s);
+
 constexpr int kCopyPairs = 480;  // page copies of one launch (by value)
 struct CopyArgs {
   uint8_t* pages;
   size_t page_bytes, layer_bytes;
+  uint64_t layers[kMaxLayers / 64];  // bit l: layer l takes part
   int n_layers, n;
-  int32_t src[kCopyPairs], dst[kCopyPairs];
+  int32_t src[kCopyPairs], dst[kCopyPairs];  // copies of one source next to each other
 };
-hipError_t launch_copy_pages(const CopyArgs& a, hipStream_t s);
+TSS_WEAK hipError_t launch_copy_pages(const CopyArgs& a, hipStream_t s);
 
 // Message of the calling thread's last failure outside a context
 // (tss_last_error(NULL)).

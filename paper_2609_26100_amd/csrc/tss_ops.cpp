@@ -166,6 +166,7 @@ int tss_copy_pages(void* hip_stream, const tss_paged_kv* kv, const int32_t* src,
   a.page_bytes = page_bytes(kv);
   a.layer_bytes = a.page_bytes * kv->n_pages;
   a.n_layers = kv->n_layers;
+  std::fill(a.layers, a.layers + kMaxLayers / 64, ~0ull);
   try {
     std::vector<uint8_t> use(kv->n_pages, 0);  // 1: a source, 2: a destination
     for (int i = 0; i < n; ++i) {

@@ -16,7 +16,9 @@ throughput.
 A drafter is any callable drafter(root, pos) -> (tokens, parent) with
 tokens[0] == root, parent[0] == -1 (parent None = chain), where pos counts
 the tokens generated so far.  The loop's own host work per step is a
-verify call, reading the accepted path, and list appends.
+verify call, reading the accepted path, and list appends; with `logprobs` also
+one call that computes the emitted tokens' log probabilities from the step's
+logits.
 """
 from __future__ import annotations
 
@@ -27,12 +29,40 @@ import numpy as np
 
 
 @dataclass
+class DecodeLogprobs:
+    logprob: np.ndarray            # of each generated token
+    entropy: np.ndarray            # of the distribution that it was taken from, nats
+    top_logprob: np.ndarray        # [tokens][k] alternatives, most likely first
+    top_token: np.ndarray
+
+
+class _Logprobs:
+    """Collects the log probabilities of the emitted tokens, step by step."""
+
+    def __init__(self, verifier, k):
+        self.verifier, self.k, self.parts = verifier, k, []
+
+    def add(self, n_nodes, nodes, emitted):
+        """`emitted` follow `nodes` of the last verify, which had n_nodes."""
+        given = np.full(n_nodes, -1, dtype=np.int32)
+        given[nodes] = emitted
+        lp, _, ent, tl, tt = self.verifier.logprobs(n_nodes, given, self.k)
+        none = np.empty((len(nodes), 0))
+        self.parts.append((lp[nodes], ent[nodes], tl[nodes] if self.k else none, tt[nodes] if self.k else none))
+
+    def result(self, n):
+        a, b, c, d = (np.concatenate(x)[:n] for x in zip(*self.parts))
+        return DecodeLogprobs(a, b, c.astype(np.float32), d.astype(np.int32))
+
+
+@dataclass
 class DecodeResult:
     tokens: np.ndarray             # the first max_new generated tokens
     steps: int                     # verify steps
     accept_lens: list = field(default_factory=list)  # accepted draft tokens per step
     seconds: float = 0.0           # wall time of the loop
     draft_seconds: float = 0.0     # of which in the drafter
+    logprobs: DecodeLogprobs | None = None  # of the tokens, where asked for
 
     @property
     def tokens_per_step(self):
@@ -43,12 +73,14 @@ class DecodeResult:
         return len(self.tokens) / self.seconds if self.seconds > 0 else float("nan")
 
 
-def speculative_decode(verifier, seq, root, max_new, drafter, mask=None):
+def speculative_decode(verifier, seq, root, max_new, drafter, mask=None, logprobs=None):
     """Generates at least max_new tokens after `root` (the last prompt token,
     whose K/V are not cached yet) and returns the first max_new.  Every step
     commits, so the sequence grows by accept_len + 1 per step (up to one
-    step's worth beyond max_new)."""
+    step's worth beyond max_new).  logprobs: None, or how many alternatives
+    (0 to 32) the result's log probabilities come with."""
     out, acc = [], []
+    lps = None if logprobs is None else _Logprobs(verifier, logprobs)
     t_draft = 0.0
     t0 = time.perf_counter()
     while len(out) < max_new:
@@ -62,19 +94,27 @@ def speculative_decode(verifier, seq, root, max_new, drafter, mask=None):
             else:
                 out.extend(int(tokens[j]) for j in verifier.path(0)[1:])
         out.append(int(nt))
+        if lps is not None:
+            nodes = list(range(al + 1)) if parent is None else [int(j) for j in verifier.path(0)]
+            lps.add(len(tokens), nodes, out[-al - 1:])
         acc.append(int(al))
         root = int(nt)
-    return DecodeResult(np.asarray(out[:max_new], dtype=np.int32), len(acc), acc, time.perf_counter() - t0, t_draft)
+    return DecodeResult(np.asarray(out[:max_new], dtype=np.int32), len(acc), acc, time.perf_counter() - t0, t_draft,
+                        lps.result(max_new) if lps is not None and acc else None)
 
 
-def autoregressive_decode(verifier, seq, root, max_new, mask=None):
-    """Plain greedy decoding: one committing verify of the root alone per token."""
+def autoregressive_decode(verifier, seq, root, max_new, mask=None, logprobs=None):
+    """Plain greedy decoding: one committing verify of the root alone per token (logprobs as speculative_decode)."""
     out = []
+    lps = None if logprobs is None else _Logprobs(verifier, logprobs)
     one = np.zeros(1, dtype=np.int32)
     t0 = time.perf_counter()
     for _ in range(max_new):
         one[0] = root
         _, nt = verifier.verify(seq, one, None, mask=mask, commit=True)
         out.append(int(nt))
+        if lps is not None:
+            lps.add(1, [0], [int(nt)])
         root = int(nt)
-    return DecodeResult(np.asarray(out, dtype=np.int32), max_new, [0] * max_new, time.perf_counter() - t0)
+    return DecodeResult(np.asarray(out, dtype=np.int32), max_new, [0] * max_new, time.perf_counter() - t0,
+                        logprobs=lps.result(max_new) if lps is not None and out else None)

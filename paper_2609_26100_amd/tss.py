@@ -30,7 +30,7 @@ EXPORTS = (
     "tss_tree_meta", "tss_set_launch_mode", "tss_profile_kernel", "tss_profile_read", "tss_last_error", "tss_status_string",
     "tss_destroy", "tss_get_logits_device", "tss_get_attn_split", "tss_check_kv", "tss_verify_static",
     "tss_static_workspace_bytes", "tss_bf16_to_f16", "tss_token_logprobs", "tss_token_logprobs_bytes",
-    "tss_window_attn", "tss_window_attn_bytes", "tss_copy_pages",
+    "tss_window_attn", "tss_window_attn_bytes", "tss_copy_pages", "tss_set_window", "tss_seq_fork", "tss_get_logprobs",
 )
 
 TSS_STATIC_SCRATCH_BYTES = 64 << 20
@@ -102,6 +102,9 @@ def lib():
             "tss_window_attn_bytes": (SZ, [KV, I32, I32, I32, I32, I32, I32]),
             "tss_window_attn": (ctypes.c_int, [P, KV, I32, P, ctypes.c_int64, I32, P, P, I32, I32, I32, I32, I32,
                                                ctypes.c_float, P, ctypes.c_int64, P, SZ]),
+            "tss_set_window": (ctypes.c_int, [P, I32, I32, I32]),
+            "tss_seq_fork": (ctypes.c_int, [P, I32, P, I32, I32]),
+            "tss_get_logprobs": (ctypes.c_int, [P, I32, P, I32, I32, P, P, P, P, P]),
             "tss_copy_pages": (ctypes.c_int, [P, KV, P, P, I32]),
             "tss_get_path": (ctypes.c_int, [P, I32, P, ctypes.POINTER(I32)]),
             "tss_seq_length": (ctypes.c_int, [P, I32, ctypes.POINTER(I32)]),
@@ -189,6 +192,10 @@ def tss_kv_alloc(ctx, n_seqs, max_tokens_per_seq, dev_pool, pool_bytes, page_ord
 def tss_set_skip_mask(ctx, seq, mask):
     m = None if mask is None else np.ascontiguousarray(mask, dtype=np.uint8)
     _check(lib().tss_set_skip_mask(ctx, seq, _ptr(m)), ctx, "tss_set_skip_mask")
+
+
+def tss_set_window(ctx, seq, sinks, window):
+    _check(lib().tss_set_window(ctx, seq, sinks, window), ctx, "tss_set_window")
 
 
 def tss_prefill(ctx, seq, tokens):
@@ -322,6 +329,29 @@ def tss_seq_length(ctx, seq) -> int:
 
 def tss_seq_truncate(ctx, seq, n_kv):
     _check(lib().tss_seq_truncate(ctx, seq, n_kv), ctx, "tss_seq_truncate")
+
+
+def tss_seq_fork(ctx, src, dst, n_kv):
+    d = np.ascontiguousarray(dst, dtype=np.int32)
+    _check(lib().tss_seq_fork(ctx, src, _ptr(d), d.size, n_kv), ctx, "tss_seq_fork")
+
+
+def tss_get_logprobs(ctx, n_nodes, tokens=None, top_k=0):
+    """Returns (logprob, rank, entropy, top_logprob, top_token) as numpy arrays: logprob and rank shaped as tokens
+    ([n_nodes] or [n_nodes][n], None without), entropy [n_nodes], the top ones [n_nodes][top_k] (None for top_k = 0)."""
+    t = None if tokens is None else np.ascontiguousarray(tokens, dtype=np.int32)
+    if t is not None and (t.ndim not in (1, 2) or t.shape[0] != n_nodes):
+        raise ValueError("tokens must be [n_nodes] or [n_nodes][n]")
+    n = 0 if t is None else t.size // max(n_nodes, 1)
+    lp = rank = top_lp = top_tok = None
+    if t is not None:
+        lp, rank = np.empty(t.shape, np.float32), np.empty(t.shape, np.int32)
+    ent = np.empty(max(n_nodes, 0), np.float32)
+    if top_k > 0:
+        top_lp, top_tok = np.empty((max(n_nodes, 0), top_k), np.float32), np.empty((max(n_nodes, 0), top_k), np.int32)
+    _check(lib().tss_get_logprobs(ctx, n_nodes, _ptr(t), n, top_k, _ptr(lp), _ptr(rank), _ptr(ent), _ptr(top_lp),
+                                  _ptr(top_tok)), ctx, "tss_get_logprobs")
+    return lp, rank, ent, top_lp, top_tok
 
 
 def tss_validate_tree(parent, n_nodes, max_nodes) -> int:

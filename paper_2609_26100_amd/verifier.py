@@ -62,6 +62,18 @@ class Verifier:
         L = self.shape.n_layers
         self._mask[seq] = np.zeros(L, np.uint8) if mask is None else np.asarray(mask, dtype=np.uint8).copy()
 
+    def set_window(self, seq, sinks, window):
+        """The sequence's tokens see its first `sinks` tokens and the last `window` ones (0: all; else at least 64)."""
+        abi.tss_set_window(self.ctx, seq, sinks, window)
+
+    def fork(self, src, dsts, n=None):
+        """Makes the sequences dsts (one or several) forks of src: its first n tokens (all of them by default), mask
+        and window."""
+        dsts = [int(x) for x in np.atleast_1d(np.asarray(dsts, dtype=np.int32))]
+        abi.tss_seq_fork(self.ctx, src, dsts, self.length(src) if n is None else n)
+        for x in dsts:
+            self._mask[x] = self._mask[src].copy()
+
     def prefill(self, seq, tokens):
         abi.tss_prefill(self.ctx, seq, tokens)
 
@@ -110,6 +122,11 @@ class Verifier:
         out = self.torch.empty((n_nodes, self.shape.vocab), dtype=self.torch.float32, device=self.device)
         abi.tss_get_logits_device(self.ctx, out.data_ptr(), n_nodes)
         return out
+
+    def logprobs(self, n_nodes, tokens=None, top_k=0):
+        """(logprob, rank, entropy, top_logprob, top_token) of the last verify's first n_nodes rows: of the given tokens
+        ([n_nodes] or [n_nodes][n]; outside the vocabulary: NaN and -1) and the top_k alternatives."""
+        return abi.tss_get_logprobs(self.ctx, n_nodes, tokens, top_k)
 
     def check_kv(self):
         """Raises if the KV binding is inconsistent (page table, lengths)."""
