@@ -8,17 +8,25 @@
 // the maxima, and for S, T, the ranks and the candidates of the alternatives.
 //   * Ranks: a token's rank is the number of logits that come before it: the sign
 //     of a difference each (a compare's mask in a scalar register would make the
-//     next instruction wait).
-//   * Alternatives: with W waves, every wave finds the ceil(k / W)-th largest of
-//     its lanes' maxima (its top 16 bits, by bisection over ballots).  The least
-//     of these has at least k logits at or above it, and few more.  Only
-//     threads whose maximum reaches it hold any: they are listed, all threads
-//     look through theirs, and what is found goes to a list in LDS, where each
-//     counts how many precede it.  Keys of (logit, token) are unique, so the
-//     order in which they got there does not matter.  Where too many are equal
-//     for the list, the k first are taken out one by one instead.
-// Rows of more than one chunk leave (m, S, T), counts and k keys for each chunk in the
-// workspace and a second launch joins them.
+//     next instruction wait), skipped where no logit of the wave reaches the token's.
+//   * Alternatives: the k-th largest of the threads' maxima (its top 16 bits) has
+//     at least k logits at or above it, and few more, and only threads whose maximum
+//     reaches it hold any.  Each of W waves finds the ceil(k / W)-th largest of its
+//     share by bisection over ballots, and the least of these is the cut.  The
+//     threads that reach it are listed, all threads look through their logits, and
+//     what is found goes to a list in LDS, where each counts how many precede it.
+//     Keys of (logit, token) are unique, so the order in which they got there does
+//     not matter.  Where too many are equal for the list, the cut is made finer, 8
+//     bits of the key at a time.
+// Rows of more than one chunk leave (m, S, T), counts and the top 16 bits of every
+// thread's maximum (2 bytes for 32 logits) for each chunk in the workspace, and a
+// second launch joins them: the alternatives are looked for once a row, not once a
+// chunk (20 of 2048 rows of 131072 bf16 take 21 us more than none; looked for in
+// every chunk they took 66).
+//
+// Bound by HBM for many rows without tokens or alternatives (2048 rows of 131072
+// bf16, 537 MB: 100 us, 5.4 TB/s); a token's rank adds two instructions a logit
+// (+ 30 us there, less for a likely token, whose chunks are mostly skipped).
 #include "../../include/tss.h"
 #include "tss_internal.h"
 
@@ -30,6 +38,7 @@ namespace {
 
 constexpr int kLpVals = 32;       // logits a thread holds
 constexpr int kLpList = 512;      // candidates in LDS
+constexpr int kLpHolders = 256;   // threads that are looked through
 constexpr int kLpTokens = TSS_LOGPROBS_MAX_TOKENS;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -123,14 +132,6 @@ __device__ __forceinline__ int wave_sum(int v) {
 __device__ __forceinline__ unsigned push_sign(unsigned bits, float d) {
   return __builtin_amdgcn_alignbit(bits, __float_as_uint(d), 31);
 }
-__device__ __forceinline__ u64 wave_max(u64 v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) {
-    const u64 o = __shfl_xor(v, off);
-    v = o > v ? o : v;
-  }
-  return v;
-}
 
 // What a row's (m, S, T) and a token's logit come to.
 struct RowSums {
@@ -141,13 +142,111 @@ struct RowSums {
   __device__ float entropy() const { return S == 0.f ? 0.f : logf(S) - T / S; }
 };
 
-// A chunk's share of a row in the workspace (row-major over rows and chunks):
-// floats m, S, T, then the token's counts, then k keys.
+// The chunks' shares of the rows in the workspace (row-major over rows and chunks).
 struct Parts {
-  float* sums;    // [rows * chunks][3]
-  int* counts;    // [rows * chunks][n_tokens]
-  u64* keys;      // [rows * chunks][top_k], largest first, 0 where the chunk has fewer tokens
+  float* sums;      // [rows * chunks][3]: m, S, T
+  int* counts;      // [rows * chunks][n_tokens]
+  uint16_t* tops;   // [rows * chunks][256]: top 16 bits of the key of each thread's maximum
 };
+
+// Shared by the threads that look for a row's alternatives.
+struct Search {
+  __align__(16) u64 list[kLpList];
+  int n, holders, bins[256], bin, above;
+  unsigned cut[16];
+  int holder[kLpHolders];
+};
+
+// The first k logits of a row of `tokens`, by W waves.  mine: the largest key (its top 16 bits) of
+// a share of the logits; the threads of the first `waves` waves all have some.
+// holders(cut, hold): calls hold(id) for the threads of the first launch that it knows to reach the
+// cut; logits(id, i, f): f(logit, token) for logit i < kLpVals of such a thread, if there is one;
+// each(f): f(logit, token) for this thread's share of the row; one(token): its logit.  All
+// threads call it.
+template <typename Holders, typename Logits, typename Each, typename One, typename Put>
+__device__ __forceinline__ void find_top(Search& s, int k, int tokens, unsigned mine, int W, int waves, Holders holders,
+                                         Logits logits, Each each, One one, Put put) {
+  const int tid = threadIdx.x, TH = W * 64, wave = tid >> 6;
+  for (int i = tid; i < kLpList; i += TH) s.list[i] = 0;
+  if (tid == 0) s.n = s.holders = 0;
+  unsigned cut = 0;
+  const int need = (k + waves - 1) / waves;
+#pragma unroll
+  for (int bit = 15; bit >= 0; --bit) {
+    const unsigned c = cut | (1u << bit);
+    cut = __popcll(__ballot(mine >= c)) >= need ? c : cut;
+  }
+  if ((tid & 63) == 0) s.cut[wave] = wave < waves ? cut : 0xffffu;
+  __syncthreads();
+  cut = s.cut[0];
+  for (int w = 1; w < W; ++w) cut = min(cut, s.cut[w]);
+  auto list = [&](float z, int t) {
+    const int at = atomicAdd(&s.n, 1);
+    if (at < kLpList) s.list[at] = pair_key(z, t);
+  };
+  // a cut at -inf: of the logits of -inf only those of the first k tokens
+  const unsigned none = order_key(-INFINITY);
+  const bool low = cut <= none >> 16;
+  const unsigned least = low ? none + 1 : cut << 16;
+  if (low && tid < k && tid < tokens && one(tid) == -INFINITY) list(-INFINITY, tid);
+  holders(low ? least >> 16 : cut, [&](int id) {
+    const int at = atomicAdd(&s.holders, 1);
+    if (at < kLpHolders) s.holder[at] = id;
+  });
+  __syncthreads();
+  const bool few = s.holders <= kLpHolders;
+  if (few) {
+    for (int i = tid; i < s.holders * kLpVals; i += TH)
+      logits(s.holder[i / kLpVals], i % kLpVals, [&](float z, int t) {
+        if (order_key(z) >= least) list(z, t);
+      });
+    __syncthreads();
+  }
+  if (!few || s.n > kLpList) {
+    // finer: the least prefix of the keys, 8 bits longer each time, that at least k keys reach
+    __syncthreads();
+    u64 prefix = 0;
+    int above = 0;  // keys beyond the prefix's
+    for (int shift = 56; shift >= 0; shift -= 8) {
+      for (int i = tid; i < 256; i += TH) s.bins[i] = 0;
+      __syncthreads();
+      each([&](float z, int t) {
+        const u64 key = pair_key(z, t);
+        if (shift == 56 || key >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&s.bins[(key >> shift) & 255], 1);
+      });
+      __syncthreads();
+      if (tid == 0) {
+        int b = 255, over = above;
+        while (b > 0 && over + s.bins[b] < k) over += s.bins[b--];
+        s.bin = b;
+        s.above = over;
+      }
+      __syncthreads();
+      above = s.above;
+      prefix |= (u64)s.bin << shift;
+      const int reach = above + s.bins[s.bin];
+      __syncthreads();
+      if (reach <= kLpList) break;
+    }
+    if (tid == 0) s.n = 0;
+    for (int i = tid; i < kLpList; i += TH) s.list[i] = 0;
+    __syncthreads();
+    each([&](float z, int t) {
+      if (pair_key(z, t) >= prefix) list(z, t);
+    });
+    __syncthreads();
+  }
+  const int n = min(s.n, kLpList);
+  for (int i = tid; i < n; i += TH) {
+    const u64 key = s.list[i];
+    int place = 0;
+    for (int j = 0; j < n; j += 8) {  // zeros behind the last
+#pragma unroll
+      for (int u = 0; u < 8; ++u) place += s.list[j + u] > key;
+    }
+    if (place < k) put(place, key);
+  }
+}
 
 __device__ __forceinline__ void write_token(const LogprobArgs& a, size_t at, const RowSums& r, int tok, float xt,
                                             int rank) {
@@ -166,11 +265,7 @@ __global__ __launch_bounds__(W * 64, PARTS ? 6 : 1) void k_logprobs(LogprobArgs 
   using L = Logit<TYPE>;
   constexpr int VE = 16 / L::size, NV = kLpVals / VE, TH = W * 64;
   __shared__ float s_m[W], s_S[W], s_T[W];
-  __shared__ unsigned s_key[W];
   __shared__ int s_count[W][kLpTokens];
-  __shared__ __align__(16) u64 s_list[kLpList];
-  __shared__ u64 s_best[W];
-  __shared__ int s_n, s_holders, s_holder[TH];
   const int r = blockIdx.x, chunk = PARTS ? blockIdx.y : 0;
   const int V = a.vocab, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -223,42 +318,19 @@ __global__ __launch_bounds__(W * 64, PARTS ? 6 : 1) void k_logprobs(LogprobArgs 
     tok = a.tokens[(size_t)r * a.n_tokens + lane];
     if (tok >= 0 && tok < V) xt = L::at(row, tok);
   }
-  for (int i = tid; i < kLpList; i += TH) s_list[i] = 0;
-  if (tid == 0) s_n = s_holders = 0;
 
   float lm = x[0];
 #pragma unroll
   for (int i = 1; i < kLpVals; ++i) lm = fmaxf(lm, x[i]);
   lm = lm != lm ? -INFINITY : lm;
   const float wm = wave_max(lm);
-  unsigned cut = 0;
-  if (a.top_k > 0) {
-    const unsigned k = order_key(lm);
-    const int need = (a.top_k + W - 1) / W;
-#pragma unroll
-    for (int bit = 31; bit >= 16; --bit) {
-      const unsigned c = cut | (1u << bit);
-      cut = __popcll(__ballot(k >= c)) >= need ? c : cut;
-    }
-  }
-  if (lane == 0) {
-    s_m[wave] = wm;
-    s_key[wave] = cut;
-  }
+  if (lane == 0) s_m[wave] = wm;
   __syncthreads();
   RowSums rs;
   rs.m = s_m[0];
-  cut = s_key[0];
 #pragma unroll
-  for (int w = 1; w < W; ++w) {
-    rs.m = fmaxf(rs.m, s_m[w]);
-    cut = min(cut, s_key[w]);
-  }
-  const float base = rs.base(), cut_value = key_value(cut);
-  auto list = [&](float z, int k) {
-    const int at = atomicAdd(&s_n, 1);
-    if (at < kLpList) s_list[at] = pair_key(z, k);
-  };
+  for (int w = 1; w < W; ++w) rs.m = fmaxf(rs.m, s_m[w]);
+  const float base = rs.base();
 
   // (x - m) log2 e as one fma: the rounding of m log2 e shifts all of them by
   // the same `shift`, which is taken out of the sums again
@@ -307,23 +379,28 @@ __global__ __launch_bounds__(W * 64, PARTS ? 6 : 1) void k_logprobs(LogprobArgs 
       // nothing of this wave's comes before it
     } else if (fabsf(y) < INFINITY && !odd) {
       // before the token an equal logit counts, behind it only a larger one:
-      // at least y, or at least the float after it; a block that holds the
-      // token counts as behind
-      const float same = y == 0.f ? -0.f : y;
+      // at least y, or at least the float after it
       const float up = y == 0.f ? __uint_as_float(1u) : __uint_as_float(__float_as_uint(y) + (y > 0.f ? 1u : -1u));
-      unsigned less = 0;
+      if (at < c0 || at >= c0 + TH * kLpVals) {
+        const float c = at < c0 ? up : y == 0.f ? -0.f : y;
+        unsigned less = 0;
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int t0 = token(v * VE);
-        const float c = t0 + VE <= at ? same : up;
+        for (int i = 0; i < kLpVals; ++i) less = push_sign(less, x[i] - c);
+        n = kLpVals - __popc(less);
+      } else {  // the row's chunk that holds the token; its block counts as behind it at first
+        unsigned less = 0;
 #pragma unroll
-        for (int e = 0; e < VE; ++e) less = push_sign(less, x[v * VE + e] - c);
-        if (t0 <= at && at < t0 + VE) {
+        for (int v = 0; v < NV; ++v) {
+          const int t0 = token(v * VE);
+          const float c = t0 + VE <= at ? (y == 0.f ? -0.f : y) : up;
 #pragma unroll
-          for (int e = 0; e < VE; ++e) n += x[v * VE + e] == y && t0 + e < at;
+          for (int e = 0; e < VE; ++e) less = push_sign(less, x[v * VE + e] - c);
         }
+        n = kLpVals - __popc(less);
+        const int blk = (at + skew) / VE;  // the thread that has it looks again at what stands before it
+        if (blk % TH == tid)
+          for (int k = max(0, blk * VE - skew); k < at; ++k) n += L::at(row, k) == y;
       }
-      n += 32 - __popc(less);
     } else {
       each([&](float z, int k) { n += pair_key(z, k) > pair_key(y, at); });
     }
@@ -333,19 +410,6 @@ __global__ __launch_bounds__(W * 64, PARTS ? 6 : 1) void k_logprobs(LogprobArgs 
   if (lane == 0) {
     s_S[wave] = S;
     s_T[wave] = T;
-  }
-  if (a.top_k > 0) {
-    // what is at or above the cut: first the threads that hold such a logit,
-    // few, whose logits all threads then share out.  Where the cut is at -inf,
-    // of the logits of -inf only the chunk's first top_k tokens
-    if (cut > order_key(-INFINITY) && !odd) {
-      if (!(lm < cut_value)) s_holder[atomicAdd(&s_holders, 1)] = tid;
-    } else {
-      const int early = max(0, c0) + a.top_k;
-      each([&](float z, int k) {
-        if (order_key(z) >= cut && (z != -INFINITY || k < early)) list(z, k);
-      });
-    }
   }
   __syncthreads();
   rs.S = s_S[0];
@@ -375,54 +439,33 @@ __global__ __launch_bounds__(W * 64, PARTS ? 6 : 1) void k_logprobs(LogprobArgs 
     }
   }
   if (a.top_k == 0) return;
-  for (int i = tid; i < s_holders * kLpVals; i += TH) {
-    const int j = i % kLpVals, h = s_holder[i / kLpVals];
-    const int k = (chunk * (TH * NV) + h + j / VE * TH) * VE + j % VE - skew;
-    if (k < 0 || k >= V) continue;
-    const float z = L::at(row, k);
-    if (!(z < cut_value)) list(z, k);
+  unsigned top = order_key(lm) >> 16;
+  if (odd) {  // NaN orders as the largest (infinities leave NaN in the sums as well)
+    bool nan = false;
+    each([&](float z, int) { nan |= z != z; });
+    if (nan) top = 0xffffu;
   }
-  __syncthreads();
-  auto put = [&](int place, u64 key) {
-    if constexpr (PARTS)
-      parts.keys[part * a.top_k + place] = key;
-    else
-      write_top(a, (size_t)r * a.top_k + place, rs, key);
-  };
-  const int n = s_n;
-  if (n <= kLpList) {
-    for (int i = tid; i < n; i += TH) {
-      const u64 k = s_list[i];
-      int place = 0;
-      for (int j = 0; j < n; j += 8) {  // zeros behind the last
-#pragma unroll
-        for (int u = 0; u < 8; ++u) place += s_list[j + u] > k;
-      }
-      if (place < a.top_k) put(place, k);
-    }
-    for (int i = n + tid; i < a.top_k; i += TH) put(i, 0);
-    return;
-  }
-  // one by one: every thread's largest key below those taken, the largest of them
-  u64 mine = 0, taken = ~0ull;
-  bool stale = true;
-  for (int t = 0; t < a.top_k; ++t) {
-    if (stale) {
-      mine = 0;
-      each([&](float z, int token) {
-        const u64 k = pair_key(z, token);
-        if (k < taken && k > mine) mine = k;
-      });
-    }
-    const u64 best = wave_max(mine);
-    __syncthreads();
-    if (lane == 0) s_best[wave] = best;
-    __syncthreads();
-    taken = s_best[0];
-#pragma unroll
-    for (int w = 1; w < W; ++w) taken = s_best[w] > taken ? s_best[w] : taken;
-    stale = mine == taken;
-    if (tid == 0) put(t, taken);
+  if constexpr (PARTS) {
+    static_assert(TH == 256, "as Parts has it");
+    parts.tops[part * TH + tid] = (uint16_t)top;
+  } else {
+    __shared__ Search s;
+    auto get = [&](int id, int i, auto f) {
+      const int k = (id + i / VE * TH) * VE + i % VE - skew;
+      if (k >= 0 && k < V) f(L::at(row, k), k);
+    };
+    auto all = [&](auto f) {
+#pragma unroll 8
+      for (int i = 0; i < kLpVals; ++i) get(tid, i, f);
+    };
+    // waves whose threads all have some of the row (at least the first)
+    const int waves = max(1, min(W, (V + skew) / VE / 64));
+    find_top(s, a.top_k, V, top, W, waves,
+             [&](unsigned cut, auto hold) {
+               if (top >= cut) hold(tid);
+             },
+             get, all, [&](int t) { return L::at(row, t); },
+             [&](int place, u64 key) { write_top(a, (size_t)r * a.top_k + place, rs, key); });
   }
 }
 
@@ -437,16 +480,30 @@ template <int TYPE>
 __global__ __launch_bounds__(256) void k_logprobs_join(LogprobArgs a, Parts parts, int chunks) {
   using L = Logit<TYPE>;
   const int r = blockIdx.x, tid = threadIdx.x, k = a.top_k;
-  extern __shared__ u64 keys[];  // [chunks][k]
   const size_t part = (size_t)r * chunks;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  for (int i = tid; i < chunks * k; i += 256) keys[i] = parts.keys[part * k + i];
+  __shared__ Search s;
+  constexpr int VE = 16 / L::size, TH = 256, NV = kLpVals / VE;
+  const int V = a.vocab;
+  const uint8_t* row = (const uint8_t*)a.x + (size_t)r * a.stride * L::size;
+  const int skew = (int)(((uintptr_t)row & 15) / L::size);
+  // thread h of chunk c is id c * 256 + h; a thread here has eight next to each other at a time
+  const uint4* tops = (const uint4*)(parts.tops + part * TH);
+  auto eights = [&](auto f) {
+    for (int i = tid; i < chunks * TH / 8; i += 256) {
+      const uint4 t = tops[i];
+      const unsigned w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+      for (int u = 0; u < 8; ++u) f(i * 8 + u, u & 1 ? w[u >> 1] >> 16 : w[u >> 1] & 0xffffu);
+    }
+  };
+  unsigned top = 0;
+  if (k > 0) eights([&](int, unsigned t) { top = max(top, t); });
   int tok = -1;
   float xt = 0.f;
   if (lane < a.n_tokens) {
     tok = a.tokens[(size_t)r * a.n_tokens + lane];
-    const void* row = (const uint8_t*)a.x + (size_t)r * a.stride * L::size;
-    if (tok >= 0 && tok < a.vocab) xt = L::at(row, tok);
+    if (tok >= 0 && tok < a.vocab) xt = L::at((const uint8_t*)a.x + (size_t)r * a.stride * L::size, tok);
   }
   // every wave sums all chunks, a lane each
   float m = -INFINITY, S = 0.f, T = 0.f;
@@ -471,27 +528,23 @@ __global__ __launch_bounds__(256) void k_logprobs_join(LogprobArgs a, Parts part
     n = wave_sum(n);
     if (lane == t) write_token(a, (size_t)r * a.n_tokens + t, rs, tok, xt, n);
   }
-  __syncthreads();
-  // a key's place: its place in its own chunk, and the keys before it in the
-  // others, whose lists are in order
-  for (int i = tid; i < chunks * k; i += 256) {
-    const u64 key = keys[i];
-    const int own = i / k;
-    int place = i % k;
-    for (int c = 0; c < chunks && place < k; ++c) {
-      if (c == own) continue;
-      int lo = 0, hi = k;
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (keys[c * k + mid] > key)
-          lo = mid + 1;
-        else
-          hi = mid;
-      }
-      place += lo;
-    }
-    if (key != 0 && place < k) write_top(a, (size_t)r * k + place, rs, key);
-  }
+  if (k == 0) return;
+  auto get = [&](int id, int i, auto f) {
+    const int t = (id / TH * (TH * NV) + id % TH + i / VE * TH) * VE + i % VE - skew;
+    if (t >= 0 && t < V) f(L::at(row, t), t);
+  };
+  auto all = [&](auto f) {
+#pragma unroll 8
+    for (int t = tid; t < V; t += 256) f(L::at(row, t), t);
+  };
+  find_top(s, k, V, top, 4, max(1, min(4, chunks / 2)),
+           [&](unsigned cut, auto hold) {
+             eights([&](int id, unsigned t) {
+               if (t >= cut) hold(id);
+             });
+           },
+           get, all, [&](int t) { return L::at(row, t); },
+           [&](int place, u64 key) { write_top(a, (size_t)r * k + place, rs, key); });
 }
 
 // Chunks of a row: one where a workgroup of up to 1024 threads holds it all (the
@@ -518,7 +571,7 @@ bool logprobs_fit(int rows, int vocab) {
 size_t logprobs_bytes(int rows, int vocab, int n_tokens, int top_k) {
   const size_t chunks = plan(vocab, 7).chunks, c = chunks * rows;
   if (chunks == 1) return 0;
-  return align16(c * 12) + align16(c * n_tokens * 4) + c * top_k * 8;
+  return align16(c * 12) + align16(c * n_tokens * 4) + (top_k > 0 ? c * 512 : 0);
 }
 
 template <int TYPE>
@@ -532,10 +585,10 @@ static hipError_t launch_typed(const LogprobArgs& a, uint8_t* ws, hipStream_t s)
     const size_t c = (size_t)p.chunks * a.rows;
     parts.sums = (float*)ws;
     parts.counts = (int*)(ws + align16(c * 12));
-    parts.keys = (u64*)(ws + align16(c * 12) + align16(c * a.n_tokens * 4));
+    parts.tops = (uint16_t*)(ws + align16(c * 12) + align16(c * a.n_tokens * 4));
     TSS_LAUNCH((k_logprobs<TYPE, 4, true>), grid, dim3(256), 0, s, a, parts, p.chunks);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    TSS_LAUNCH(k_logprobs_join<TYPE>, dim3(a.rows), dim3(256), (size_t)p.chunks * a.top_k * 8, s, a, parts, p.chunks);
+    TSS_LAUNCH(k_logprobs_join<TYPE>, dim3(a.rows), dim3(256), 0, s, a, parts, p.chunks);
   } else if (p.waves == 4) {
     TSS_LAUNCH((k_logprobs<TYPE, 4, false>), grid, dim3(256), 0, s, a, parts, p.chunks);
   } else if (p.waves == 8) {
