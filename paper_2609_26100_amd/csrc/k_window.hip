@@ -503,20 +503,22 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(A a, int split
 
 // --- many rows (fp16) --------------------------------------------------------------
 
-constexpr int kRowsWaves = 4, kRowsPages = 4, kRowsStages = 2;
+constexpr int kRowsPages = 4, kRowsStages = 2;
 
-// Four waves of TILES 16-row tiles walk the pages together, four pages a step,
-// one loaded by each wave into an LDS ring by global -> LDS loads, two steps in flight.
+// WAVES waves of TILES 16-row tiles walk the pages together, four pages a step,
+// loaded into an LDS ring by global -> LDS loads, two steps in flight: a page by each of
+// four waves, K or V of one by each of eight.
 // K chunk c covers dims 32 c .. + 31 (16 tokens x 64 bytes of a page), V chunk i
 // dims 32 i .. + 31 of four token groups (4 x 256 bytes): each is one KiB load, read
 // back lane by lane in order.  grid as k_window_few.
-template <int HD, int TILES, typename A>
-__global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(A a, int splits, int blocks, float* part_o,
+template <int HD, int WAVES, int TILES, typename A>
+__global__ __launch_bounds__(WAVES * 64, 2) void k_window_rows(A a, int splits, int blocks, float* part_o,
                                                                     float* part_ml) {
   constexpr int NK = HD / 32;              // KiB of a K (or V) page block
   constexpr int PW = 2 * NK;               // loads of one wave per step: one page
   constexpr int STAGE = kRowsPages * 2 * NK * 1024;
-  constexpr int ROWS = kRowsWaves * TILES * 16;
+  constexpr int ROWS = WAVES * TILES * 16;
+  static_assert(WAVES == kRowsPages || WAVES == 2 * kRowsPages, "a page, or K or V of one, a wave");
   __shared__ __align__(16) uint8_t ring[kRowsStages * STAGE];
   const int head = blockIdx.x % a.n_heads;
   // the last rows first: without a window theirs is the longest walk
@@ -531,7 +533,7 @@ __global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(A a, int spl
   if (head == 0 && blockIdx.z == 0 && threadIdx.x == 0)
     report(a, b, blockIdx.y, block, blocks, max(1, (steps + per - 1) / per));
   if (n_st == 0 && blockIdx.z > 0) {  // nothing left for this split
-    for (int i = threadIdx.x; i < b.n_v; i += kRowsWaves * 64)
+    for (int i = threadIdx.x; i < b.n_v; i += WAVES * 64)
       *(float2*)(part_ml + part_slot(a, b, b.v0 + i, head, blockIdx.z) * 2) = make_float2(kLowest, 0.f);
     return;
   }
@@ -557,14 +559,19 @@ __global__ __launch_bounds__(kRowsWaves * 64, 2) void k_window_rows(A a, int spl
     ids = there ? id : 0;
   };
   auto issue = [&](int st) {
-    const int phys = __builtin_amdgcn_readlane(ids, (st * kRowsPages + wave) & 63);
+    const int page = wave % kRowsPages;
+    const int phys = __builtin_amdgcn_readlane(ids, (st * kRowsPages + page) & 63);
     const uint8_t* kb = page_k<_Float16, HD>(a, phys, head);
     const uint8_t* vb = kb + (size_t)a.n_heads * (kPage * HD * 2);
-    const unsigned dst = lds0 + (unsigned)((st % kRowsStages) * STAGE + wave * 2 * NK * 1024);
+    const unsigned dst = lds0 + (unsigned)((st % kRowsStages) * STAGE + page * 2 * NK * 1024);
+    if (wave < kRowsPages) {
 #pragma unroll
-    for (int c = 0; c < NK; ++c) dma_kib(kb, koff + c * 64u, dst + c * 1024u);
+      for (int c = 0; c < NK; ++c) dma_kib(kb, koff + c * 64u, dst + c * 1024u);
+    }
+    if (WAVES == kRowsPages || wave >= kRowsPages) {
 #pragma unroll
-    for (int c = 0; c < NK; ++c) dma_kib(vb, voff + c * 256u, dst + (NK + c) * 1024u);
+      for (int c = 0; c < NK; ++c) dma_kib(vb, voff + c * 256u, dst + (NK + c) * 1024u);
+    }
   };
 
   f16x8 q[TILES][NK];
@@ -800,12 +807,17 @@ __global__ __launch_bounds__(256) void k_window_join(A a, int splits, const floa
 // most of the chip idle and each still has some pages to walk: one row over 1028
 // tokens of 32 heads 15.1 us in one split, 10.8 + 3.6 in two, 8.4 + 3.0 in four.
 struct Plan {
-  int rows, blocks, splits;
+  int rows, waves, blocks, splits;
 };
 // pages: most that a walk can have; seqs: sequences or items.
 Plan plan(bool f16, int n_heads, int64_t v_rows, int64_t seqs, int64_t pages) {
   Plan p;
-  p.rows = !f16 || v_rows <= kFewRows ? kFewRows : v_rows <= kRowsWaves * 16 ? kRowsWaves * 16 : kRowsWaves * 32;
+  p.rows = !f16 || v_rows <= kFewRows ? kFewRows : v_rows <= 64 ? 64 : 128;
+  // up to 128 rows are mostly short of their tiles (17 nodes of 4 heads a kv head are
+  // 4.25): eight waves of one tile share the work better than four of two (eight
+  // sequences of those over up to 17080 tokens 52.2 against 66.4 us, 128 prompt rows over
+  // 1155 tokens 24.0 against 26.0), which read LDS half as often in longer blocks
+  p.waves = p.rows == kFewRows ? kFewWaves : v_rows > 64 && v_rows <= 128 ? 8 : 4;
   p.blocks = (int)((v_rows + p.rows - 1) / p.rows);
   // a wave of few rows takes most of a SIMD's registers: one workgroup a CU
   const int64_t target = p.rows == kFewRows ? 256 : 512, wgs = n_heads * seqs * p.blocks;
@@ -846,10 +858,13 @@ static hipError_t launch_typed(const WindowArgs& a, float* ws, hipStream_t s) {
   if (p.rows == kFewRows) {
     TSS_LAUNCH((k_window_few<T, HD, WindowArgs>), grid, dim3(kFewWaves * 64), 0, s, a, p.splits, part_o, part_ml);
   } else if constexpr (sizeof(T) == 2) {
-    if (p.rows == kRowsWaves * 16)
-      TSS_LAUNCH((k_window_rows<HD, 1, WindowArgs>), grid, dim3(kRowsWaves * 64), 0, s, a, p.splits, p.blocks, part_o, part_ml);
+    const dim3 block(p.waves * 64);
+    if (p.rows == 64)
+      TSS_LAUNCH((k_window_rows<HD, 4, 1, WindowArgs>), grid, block, 0, s, a, p.splits, p.blocks, part_o, part_ml);
+    else if (p.waves == 8)
+      TSS_LAUNCH((k_window_rows<HD, 8, 1, WindowArgs>), grid, block, 0, s, a, p.splits, p.blocks, part_o, part_ml);
     else
-      TSS_LAUNCH((k_window_rows<HD, 2, WindowArgs>), grid, dim3(kRowsWaves * 64), 0, s, a, p.splits, p.blocks, part_o, part_ml);
+      TSS_LAUNCH((k_window_rows<HD, 4, 2, WindowArgs>), grid, block, 0, s, a, p.splits, p.blocks, part_o, part_ml);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
@@ -866,13 +881,13 @@ hipError_t launch_window(bool f16, int head_dim, const WindowArgs& a, void* work
 
 hipError_t launch_window_pass(int head_dim, const WindowPassArgs& a, hipStream_t s) {
   if (a.rows < 1 || a.rows > kPromptRows) return hipErrorInvalidValue;
-  const int blocks = (a.rows + kRowsWaves * 32 - 1) / (kRowsWaves * 32);  // passes take more than 64 rows
-  const dim3 grid(a.n_heads * blocks, 1, 1), block(kRowsWaves * 64);
+  const int blocks = (a.rows + 127) / 128;  // passes take more than 64 rows
+  const dim3 grid(a.n_heads * blocks, 1, 1), block(4 * 64);
   float* none = nullptr;
   if (head_dim == 128)
-    TSS_LAUNCH((k_window_rows<128, 2, WindowPassArgs>), grid, block, 0, s, a, 1, blocks, none, none);
+    TSS_LAUNCH((k_window_rows<128, 4, 2, WindowPassArgs>), grid, block, 0, s, a, 1, blocks, none, none);
   else
-    TSS_LAUNCH((k_window_rows<64, 2, WindowPassArgs>), grid, block, 0, s, a, 1, blocks, none, none);
+    TSS_LAUNCH((k_window_rows<64, 4, 2, WindowPassArgs>), grid, block, 0, s, a, 1, blocks, none, none);
   return hipGetLastError();
 }
 
@@ -887,15 +902,14 @@ static hipError_t launch_step_typed(int n_items, const WindowStepArgs& a, float*
     pages = std::max(pages, walk_pages(it.slots, a.max_length, it.sinks, it.window == INT_MAX ? 0 : it.window));
   }
   Plan p = plan(sizeof(T) == 2, a.n_heads, rows, n_items, pages);
-  if (p.rows > kRowsWaves * 16) return hipErrorInvalidValue;  // items have at most 64 rows
+  if (p.rows > 64) return hipErrorInvalidValue;  // items have at most 64 rows
   // a slot holds 64 rows of one head
   p.splits = (int)std::min<int64_t>(p.splits, std::max<int64_t>(1, part_slots * 64 / ((int64_t)a.rows * a.n_heads)));
   const dim3 grid(a.n_heads * p.blocks, n_items, p.splits);
   if (p.rows == kFewRows)
     TSS_LAUNCH((k_window_few<T, HD, WindowStepArgs>), grid, dim3(kFewWaves * 64), 0, s, a, p.splits, part_o, part_ml);
   else if constexpr (sizeof(T) == 2)
-    TSS_LAUNCH((k_window_rows<HD, 1, WindowStepArgs>), grid, dim3(kRowsWaves * 64), 0, s, a, p.splits, p.blocks, part_o,
-               part_ml);
+    TSS_LAUNCH((k_window_rows<HD, 4, 1, WindowStepArgs>), grid, dim3(4 * 64), 0, s, a, p.splits, p.blocks, part_o, part_ml);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   // the timing of a launch is that of the one above
