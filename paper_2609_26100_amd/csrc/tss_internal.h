@@ -422,6 +422,9 @@ hipError_t init_prompt_attributes();
 hipError_t launch_rope_table(float2* tab, int max_pos, int head_dim, float base, hipStream_t s);
 
 // The operators on the caller's tensors (tss_ops.cpp checks their arguments).
+// What the host runtime calls of them is weak: it also links without their kernels
+// (its sanitizer build), where a call that needs one is refused.
+#define TSS_WEAK __attribute__((weak))
 struct LogprobArgs {
   const void* x;           // [rows][vocab], rows `stride` elements apart
   int64_t stride;
@@ -436,9 +439,9 @@ struct LogprobArgs {
 };
 // Limits of a call: logprobs_fit is whether its workgroups can be launched.
 constexpr int kLogprobVocab = 1 << 20;
-__attribute__((weak)) bool logprobs_fit(int rows, int vocab);
-__attribute__((weak)) size_t logprobs_bytes(int rows, int vocab, int n_tokens, int top_k);
-__attribute__((weak)) hipError_t launch_logprobs(const LogprobArgs& a, void* workspace, hipStream_t s);
+TSS_WEAK bool logprobs_fit(int rows, int vocab);
+TSS_WEAK size_t logprobs_bytes(int rows, int vocab, int n_tokens, int top_k);
+TSS_WEAK hipError_t launch_logprobs(const LogprobArgs& a, void* workspace, hipStream_t s);
 
 struct WindowArgs {
   const void* q;           // [rows][n_q_heads][hd], rows q_stride elements apart
@@ -475,10 +478,8 @@ struct WindowStepArgs : WindowArgs {
   } item[kAttnMaxItems];
   int32_t pt_off[kMaxSegs];
 };
-// part: scratch of part_slots * 64 * (hd + 2) floats, as the attention of a step has it.
-// Weak, as the calls below: the host runtime also links without the operators'
-// kernels (its sanitizer build); a call that needs one is then refused.
-#define TSS_WEAK __attribute__((weak))
+// part_o, part_ml: scratch of part_slots slots of 64 rows of one head, as the attention
+// of a step has it.
 TSS_WEAK hipError_t launch_window_pass(int head_dim, const WindowPassArgs& a, hipStream_t s);
 TSS_WEAK hipError_t launch_window_step(bool f16, int head_dim, int n_items, const WindowStepArgs& a, float* part_o,
                                        float* part_ml, size_t part_slots, hipStream_t s);

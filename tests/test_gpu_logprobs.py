@@ -118,6 +118,18 @@ def test_ties_and_special_rows(kind, vocab):
         check(x, tok, top, ops.token_logprobs(x, tok, top))
 
 
+def test_logits_beyond_4_gib():
+    rows, vocab = 18000, 131075                  # 4.7 GB, rows that are not aligned
+    x = torch.zeros(rows, vocab, dtype=torch.bfloat16, device=DEV)
+    x[-40:] = logits(40, vocab, "bf16", 9)
+    tok = torch.full((rows, 2), 3, dtype=torch.int32, device=DEV)
+    got = ops.token_logprobs(x, tok, 4)
+    tail = ops.TokenLogprobs(*(t[-40:] for t in got))
+    check(x[-40:], tok[-40:], 4, tail)
+    flat = ops.TokenLogprobs(*(t[:2] for t in got))  # all equal: the first tokens, each 1 / vocab
+    check(x[:2], tok[:2], 4, flat)
+
+
 def test_the_same_bits_every_time():
     x = logits(40, 32000, "f32", 11)
     tok = torch.arange(40, dtype=torch.int32, device=DEV)

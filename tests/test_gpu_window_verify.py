@@ -160,6 +160,24 @@ def test_sweep_under_a_window(models):
                                                           dense_context=True))
 
 
+def test_timing_of_windowed_attention(models):
+    """One attention launch a step is timed, its merge launch is not taken for another."""
+    v, _ = models("bf16")
+    start(v, 0, synth.context_tokens(SMALL.vocab, 1500, stream=145), 4, 1000)
+    draft = synth.context_tokens(SMALL.vocab, 40, stream=146)
+    v.verify(0, draft)
+    want = v.logits(40)
+    abi.tss_profile_kernel(v.ctx, abi.TSS_K_ATTN, 1)
+    abi.tss_profile_read(v.ctx, reset=True)
+    for _ in range(3):
+        v.verify(0, draft)
+    ms, n = abi.tss_profile_read(v.ctx, reset=True)
+    abi.tss_profile_kernel(v.ctx, -1)
+    assert n == 3 and 0 < ms < 3
+    assert v.attn_split()[0][0] > 1              # merged across workgroups
+    np.testing.assert_array_equal(v.logits(40), want)
+
+
 def test_window_refusals(models):
     v, _ = models("f32")
     for bad in ((0, -1, 64), (0, 0, -1), (0, 0, 63), (0, 4, 1), (99, 0, 64), (-1, 0, 64)):
