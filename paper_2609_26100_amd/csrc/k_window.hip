@@ -39,7 +39,10 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMaxSplits = 64;
-constexpr int kLeastPages = 16;  // pages that a split has at least
+// Pages that a split has at least: two steps of four pages for the kernel of many
+// rows (33 rows over 500 tokens of 32 heads 11.0 us, with sixteen 13.2; 500 rows of 8
+// heads 18.3 and 21.0), two for each of eight waves for that of few.
+constexpr int kFewLeast = 16, kRowsLeast = 8;
 constexpr float kLowest = -3e38f;  // running maximum of a row that has seen nothing
 // A row's reference maximum is raised where the scores exceed it by this (in
 // powers of two): probabilities up to 2^8 of the largest fit fp16 as well as
@@ -246,7 +249,7 @@ __device__ __forceinline__ void report(const WindowStepArgs& a, const Block& b, 
 
 // Words of a lane's V piece (tokens 0, 1 and 2, 3 of its group) that are kept.
 __device__ __forceinline__ uint2 keep16(const Block& b, int t, bool there) {
-  auto half = [&](int u) { return there & b.live(t + u) ? 0xffffu : 0u; };
+  auto half = [&](int u) { return (there & b.live(t + u)) ? 0xffffu : 0u; };
   return uint2{half(0) | half(1) << 16, half(2) | half(3) << 16};
 }
 
@@ -337,7 +340,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(A a, int split
   const int full_sinks = b.sinks / kPage;
 
   // this split's pages, from `from`; wave w takes steps w, w + 8, ...
-  const int steps = (b.n_pages + PP - 1) / PP, per = split_steps(steps, splits, kLeastPages / PP);
+  const int steps = (b.n_pages + PP - 1) / PP, per = split_steps(steps, splits, kFewLeast / PP);
   const int st0 = blockIdx.z * per, n_st = min(per, steps - st0);
   if (head == 0 && blockIdx.z == 0 && tid == 0)
     report(a, b, blockIdx.y, blockIdx.x / a.n_heads, gridDim.x / a.n_heads, max(1, (steps + per - 1) / per));
@@ -415,7 +418,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(A a, int split
 #pragma unroll
           for (int i = 0; i < N; ++i) pg[p].v[i] = both(pg[p].v[i], uint4{k.x, k.y, k.x, k.y});
         } else {
-          auto word = [&](int u) { return pg[p].there & b.live(t + u) ? ~0u : 0u; };
+          auto word = [&](int u) { return (pg[p].there & b.live(t + u)) ? ~0u : 0u; };
           const uint4 k = {word(0), word(1), word(2), word(3)};
 #pragma unroll
           for (int i = 0; i < N; ++i) pg[p].v[i] = both(pg[p].v[i], k);
@@ -528,7 +531,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_window_rows(A a, int splits, 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int r16 = lane & 15, grp = lane >> 4;
   const int steps = (b.n_pages + kRowsPages - 1) / kRowsPages;
-  const int per = split_steps(steps, splits, kLeastPages / kRowsPages);
+  const int per = split_steps(steps, splits, kRowsLeast / kRowsPages);
   const int st0 = blockIdx.z * per, n_st = max(0, min(per, steps - st0));
   if (head == 0 && blockIdx.z == 0 && threadIdx.x == 0)
     report(a, b, blockIdx.y, block, blocks, max(1, (steps + per - 1) / per));
@@ -623,6 +626,14 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_window_rows(A a, int splits, 
         for (int t = 0; t < TILES; ++t) S[t][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[t][c], S[t][p], 0, 0, 0);
       }
     }
+    // V is requested before the softmax, whose instructions hide it; the empty asm
+    // keeps the compiler from moving the reads down to their use
+    uint4 V[kRowsPages][NK];
+#pragma unroll
+    for (int p = 0; p < kRowsPages; ++p)
+#pragma unroll
+      for (int i = 0; i < NK; ++i) V[p][i] = *(const uint4*)(base + (p * 2 * NK + NK + i) * 1024);
+    asm volatile("" ::: "memory");
     const bool whole = i1 <= span.all_last && (i1 < full_sinks || i0 >= span.all_first);
     if (EDGE || !whole) {
 #pragma unroll
@@ -676,8 +687,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_window_rows(A a, int splits, 
     for (int h = 0; h < kRowsPages / 2; ++h)
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
-        uint4 va = *(const uint4*)(base + (4 * h * NK + NK + i) * 1024);
-        uint4 vb = *(const uint4*)(base + ((4 * h + 2) * NK + NK + i) * 1024);
+        uint4 va = V[2 * h][i], vb = V[2 * h + 1][i];
         if constexpr (EDGE) {
           va = both(va, keep[2 * h]);
           vb = both(vb, keep[2 * h + 1]);
@@ -779,7 +789,8 @@ __global__ __launch_bounds__(256) void k_window_join(A a, int splits, const floa
   float top = ml.x, L;
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-  const float f = __builtin_amdgcn_exp2f(ml.x - top);
+  // a split that saw nothing has weight 0: it may have written no output
+  const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
   L = f * ml.y;
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) L += __shfl_xor(L, off);
@@ -790,7 +801,7 @@ __global__ __launch_bounds__(256) void k_window_join(A a, int splits, const floa
     if (g >= splits) break;
     const float w = __shfl(f, g);
 #pragma unroll
-    for (int n = 0; n < N; ++n) o[n] += w == 0.f ? 0.f : w * p[i][n];  // a split without pages has written no output
+    for (int n = 0; n < N; ++n) o[n] += w == 0.f ? 0.f : w * p[i][n];
   }
 #pragma unroll
   for (int n = 0; n < N; ++n) s_o[wave][lane * N + n] = o[n];
@@ -800,6 +811,50 @@ __global__ __launch_bounds__(256) void k_window_join(A a, int splits, const floa
     const float x = (s_o[0][d] + s_o[1][d]) + (s_o[2][d] + s_o[3][d]);
     *out_at<T, HD>(a, row, qh, d) = (T)(x * (L > 0.f ? 1.f / L : L));
   }
+}
+
+// The same by a wave for each (row, query head), for at most sixteen splits: after the
+// kernel of many rows, whose pairs fill the chip by themselves (300 rows of 32 heads
+// over 700 tokens 29.1 -> 25.7 us with the kernel before it, 20 rows of each of 4
+// sequences over 300 13.6 -> 13.0; after that of few rows the workgroup is ahead, 9
+// rows each of 8 sequences over 2048 tokens 20.4 against 20.8).
+// grid (rows of a sequence, sequence, query heads / 4).
+constexpr int kWaveSplits = 16;
+template <int HD, typename A>
+__global__ __launch_bounds__(256) void k_window_join_wave(A a, int splits, const float* part_o, const float* part_ml) {
+  constexpr int N = HD / 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int heads = a.n_heads * a.group, qh = blockIdx.z * 4 + wave;
+  const int row = join_row(a, blockIdx.y, blockIdx.x);
+  if (row < 0 || qh >= heads) return;
+  const size_t slot = (size_t)row * heads + qh, stride = (size_t)a.rows * heads;
+  float2 ml = make_float2(kLowest, 0.f);
+  if (lane < splits) ml = *(const float2*)(part_ml + (slot + lane * stride) * 2);
+  float p[kWaveSplits][N];
+#pragma unroll
+  for (int i = 0; i < kWaveSplits; ++i) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) p[i][n] = i < splits ? part_o[(slot + i * stride) * HD + lane * N + n] : 0.f;
+  }
+  float top = ml.x, L;
+#pragma unroll
+  for (int off = 8; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+  // a split that saw nothing has weight 0: it may have written no output
+  const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+  L = f * ml.y;
+#pragma unroll
+  for (int off = 8; off >= 1; off >>= 1) L += __shfl_xor(L, off);
+  L = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(L)));
+  const float inv = L > 0.f ? 1.f / L : L;
+  float o[N] = {};
+#pragma unroll
+  for (int i = 0; i < kWaveSplits; ++i) {
+    const float g = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
+#pragma unroll
+    for (int n = 0; n < N; ++n) o[n] += i < splits && g != 0.f ? g * p[i][n] : 0.f;
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) *out_at<_Float16, HD>(a, row, qh, lane * N + n) = (_Float16)(o[n] * inv);
 }
 
 // How a launch is cut up: virtual rows of a block, blocks of a sequence, splits of
@@ -821,9 +876,24 @@ Plan plan(bool f16, int n_heads, int64_t v_rows, int64_t seqs, int64_t pages) {
   p.blocks = (int)((v_rows + p.rows - 1) / p.rows);
   // a wave of few rows takes most of a SIMD's registers: one workgroup a CU
   const int64_t target = p.rows == kFewRows ? 256 : 512, wgs = n_heads * seqs * p.blocks;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, target / wgs, pages / kLeastPages}));
+  const int64_t least = p.rows == kFewRows ? kFewLeast : kRowsLeast;
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, target / wgs, pages / least}));
   return p;
 }
+
+template <typename T, int HD, typename A>
+void launch_join(const A& a, int rows, int seqs, const Plan& p, const float* part_o, const float* part_ml,
+                 hipStream_t s) {
+  const int heads = a.n_heads * a.group;
+  if constexpr (std::is_same<T, _Float16>::value)
+    if (p.rows != kFewRows && p.splits <= kWaveSplits) {
+      TSS_LAUNCH((k_window_join_wave<HD, A>), dim3(rows, seqs, (heads + 3) / 4), dim3(256), 0, s, a, p.splits, part_o,
+                 part_ml);
+      return;
+    }
+  TSS_LAUNCH((k_window_join<T, HD, A>), dim3(rows, seqs, heads), dim3(256), 0, s, a, p.splits, part_o, part_ml);
+}
+
 // Pages that a block of `rows` rows walks at most.
 int64_t walk_pages(int64_t rows, int64_t max_length, int64_t sinks, int64_t window) {
   const int64_t all = (max_length + kPage - 1) / kPage;
@@ -868,8 +938,7 @@ static hipError_t launch_typed(const WindowArgs& a, float* ws, hipStream_t s) {
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  TSS_LAUNCH((k_window_join<T, HD, WindowArgs>), dim3(a.max_rows, a.n_seqs, a.n_heads * a.group), dim3(256), 0, s, a,
-             p.splits, part_o, part_ml);
+  launch_join<T, HD>(a, a.max_rows, a.n_seqs, p, part_o, part_ml, s);
   return hipGetLastError();
 }
 
@@ -915,8 +984,7 @@ static hipError_t launch_step_typed(int n_items, const WindowStepArgs& a, float*
   // the timing of a launch is that of the one above
   const LaunchTiming timing = launch_timing();
   launch_timing() = LaunchTiming{};
-  TSS_LAUNCH((k_window_join<T, HD, WindowStepArgs>), dim3(rows, n_items, a.n_heads), dim3(256), 0, s, a, p.splits, part_o,
-             part_ml);
+  launch_join<T, HD>(a, (int)rows, n_items, p, part_o, part_ml, s);
   launch_timing() = timing;
   return hipGetLastError();
 }

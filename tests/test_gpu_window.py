@@ -155,6 +155,20 @@ def test_rows_that_see_nothing_and_rows_behind(kind):
     assert ((out[7:9].double().cpu() - want).abs() <= bound).all()
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("rows", [[2, 2], [30, 30]])
+def test_rows_that_see_nothing_where_others_are_split(kind, rows, monkeypatch):
+    """A sequence without tokens beside a long one, whose pages are split: zeros, whatever the workspace held."""
+    c = Cache([0, 3000], 2, 128, kind, 57)
+    q = queries(rows, 2, 128, kind, 57)
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: empty(*a, **k).fill_(255 if k["dtype"] == torch.uint8 else 7))
+    out = ops.window_attention(q.to(DEV), c.pool, c.table, offsets(rows), c.lengths, 0, 0)
+    assert (out[:rows[0]] == 0).all()
+    want, bound = ref.attention(q[rows[0]:], *c.kv[1], ref.visible(rows[1], 3000, 0, 0))
+    assert ((out[rows[0]:].double().cpu() - want).abs() <= bound).all()
+
+
 def test_lengths_beyond_the_table_count_as_its_tokens():
     c = Cache([48], 2, 64, "f16", 53)
     c.table = c.table[:, :3].contiguous()
