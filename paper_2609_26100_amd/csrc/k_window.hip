@@ -18,8 +18,15 @@
 // Two kernels: few rows (up to 16) are bound by the cache's bytes, so each wave
 // streams pages of its own into registers and the waves' states meet at the end;
 // many rows share each page through LDS, a wave for each 16 or 32 rows.  Where
-// the blocks are too few for the chip, each block's pages are split among several workgroups
-// and a second launch joins their states.
+// the blocks are too few for the chip, each block's pages are split among several
+// workgroups and a second launch joins their states.
+//
+// Long contexts of few rows are bound by HBM (5 rows of 32 heads over 8 kv heads
+// and 100003 tokens, 410 MB: 74 + 5 us, 5.2 TB/s), short ones by their two launches
+// (one row of 32 heads over 1028 tokens 8.5 + 3.0 us).  Blocks of many rows take, for
+// each step of 64 tokens and 128 rows, 0.43 us each of a SIMD's matrix products and of
+// its LDS reads and as much of the softmax, and two waves a SIMD hide little of one
+// behind the other (2048 rows of 32 heads, 1028 tokens each: 57 us, 600 TFLOP/s).
 //
 // Tokens that no row of the block sees may hold anything: their scores are
 // replaced, and their V, which the product would multiply by 0, is cleared.
@@ -40,8 +47,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMaxSplits = 64;
 // Pages that a split has at least: two steps of four pages for the kernel of many
-// rows (33 rows over 500 tokens of 32 heads 11.0 us, with sixteen 13.2; 500 rows of 8
-// heads 18.3 and 21.0), two for each of eight waves for that of few.
+// rows (33 rows over 500 tokens of 32 heads 11.0 us, with sixteen 13.2), two for each
+// of eight waves for that of few.
 constexpr int kFewLeast = 16, kRowsLeast = 8;
 constexpr float kLowest = -3e38f;  // running maximum of a row that has seen nothing
 // A row's reference maximum is raised where the scores exceed it by this (in
@@ -508,20 +515,17 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(A a, int split
 
 constexpr int kRowsPages = 4, kRowsStages = 2;
 
-// WAVES waves of TILES 16-row tiles walk the pages together, four pages a step,
-// loaded into an LDS ring by global -> LDS loads, two steps in flight: a page by each of
-// four waves, K or V of one by each of eight.
+// Four waves of TILES 16-row tiles walk the pages together, four pages a step, one
+// loaded by each wave into an LDS ring by global -> LDS loads, two steps in flight.
 // K chunk c covers dims 32 c .. + 31 (16 tokens x 64 bytes of a page), V chunk i
 // dims 32 i .. + 31 of four token groups (4 x 256 bytes): each is one KiB load, read
 // back lane by lane in order.  grid as k_window_few.
-template <int HD, int WAVES, int TILES, typename A>
-__global__ __launch_bounds__(WAVES * 64, 2) void k_window_rows(A a, int splits, int blocks, float* part_o,
+template <int HD, int TILES, typename A>
+__global__ __launch_bounds__(kRowsPages * 64, 2) void k_window_rows(A a, int splits, int blocks, float* part_o,
                                                                     float* part_ml) {
   constexpr int NK = HD / 32;              // KiB of a K (or V) page block
-  constexpr int PW = 2 * NK;               // loads of one wave per step: one page
   constexpr int STAGE = kRowsPages * 2 * NK * 1024;
-  constexpr int ROWS = WAVES * TILES * 16;
-  static_assert(WAVES == kRowsPages || WAVES == 2 * kRowsPages, "a page, or K or V of one, a wave");
+  constexpr int ROWS = kRowsPages * TILES * 16;
   __shared__ __align__(16) uint8_t ring[kRowsStages * STAGE];
   const int head = blockIdx.x % a.n_heads;
   // the last rows first: without a window theirs is the longest walk
@@ -536,7 +540,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_window_rows(A a, int splits, 
   if (head == 0 && blockIdx.z == 0 && threadIdx.x == 0)
     report(a, b, blockIdx.y, block, blocks, max(1, (steps + per - 1) / per));
   if (n_st == 0 && blockIdx.z > 0) {  // nothing left for this split
-    for (int i = threadIdx.x; i < b.n_v; i += WAVES * 64)
+    for (int i = threadIdx.x; i < b.n_v; i += kRowsPages * 64)
       *(float2*)(part_ml + part_slot(a, b, b.v0 + i, head, blockIdx.z) * 2) = make_float2(kLowest, 0.f);
     return;
   }
@@ -562,19 +566,14 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_window_rows(A a, int splits, 
     ids = there ? id : 0;
   };
   auto issue = [&](int st) {
-    const int page = wave % kRowsPages;
-    const int phys = __builtin_amdgcn_readlane(ids, (st * kRowsPages + page) & 63);
+    const int phys = __builtin_amdgcn_readlane(ids, (st * kRowsPages + wave) & 63);
     const uint8_t* kb = page_k<_Float16, HD>(a, phys, head);
     const uint8_t* vb = kb + (size_t)a.n_heads * (kPage * HD * 2);
-    const unsigned dst = lds0 + (unsigned)((st % kRowsStages) * STAGE + page * 2 * NK * 1024);
-    if (wave < kRowsPages) {
+    const unsigned dst = lds0 + (unsigned)((st % kRowsStages) * STAGE + wave * 2 * NK * 1024);
 #pragma unroll
-      for (int c = 0; c < NK; ++c) dma_kib(kb, koff + c * 64u, dst + c * 1024u);
-    }
-    if (WAVES == kRowsPages || wave >= kRowsPages) {
+    for (int c = 0; c < NK; ++c) dma_kib(kb, koff + c * 64u, dst + c * 1024u);
 #pragma unroll
-      for (int c = 0; c < NK; ++c) dma_kib(vb, voff + c * 256u, dst + (NK + c) * 1024u);
-    }
+    for (int c = 0; c < NK; ++c) dma_kib(vb, voff + c * 256u, dst + (NK + c) * 1024u);
   };
 
   f16x8 q[TILES][NK];
@@ -815,9 +814,8 @@ __global__ __launch_bounds__(256) void k_window_join(A a, int splits, const floa
 
 // The same by a wave for each (row, query head), for at most sixteen splits: after the
 // kernel of many rows, whose pairs fill the chip by themselves (300 rows of 32 heads
-// over 700 tokens 29.1 -> 25.7 us with the kernel before it, 20 rows of each of 4
-// sequences over 300 13.6 -> 13.0; after that of few rows the workgroup is ahead, 9
-// rows each of 8 sequences over 2048 tokens 20.4 against 20.8).
+// over 700 tokens in five splits 29.1 us with workgroups, 25.7 with waves; one row over
+// 1028 tokens of 32 heads, after the kernel of few, 9.3 and 10.0).
 // grid (rows of a sequence, sequence, query heads / 4).
 constexpr int kWaveSplits = 16;
 template <int HD, typename A>
@@ -858,26 +856,44 @@ __global__ __launch_bounds__(256) void k_window_join_wave(A a, int splits, const
 }
 
 // How a launch is cut up: virtual rows of a block, blocks of a sequence, splits of
-// a block's pages.  Splits are worth their second launch where the blocks leave
-// most of the chip idle and each still has some pages to walk: one row over 1028
-// tokens of 32 heads 15.1 us in one split, 10.8 + 3.6 in two, 8.4 + 3.0 in four.
+// a block's pages.
 struct Plan {
-  int rows, waves, blocks, splits;
+  int rows, blocks, splits;
 };
 // pages: most that a walk can have; seqs: sequences or items.
 Plan plan(bool f16, int n_heads, int64_t v_rows, int64_t seqs, int64_t pages) {
   Plan p;
-  p.rows = !f16 || v_rows <= kFewRows ? kFewRows : v_rows <= 64 ? 64 : 128;
-  // up to 128 rows are mostly short of their tiles (17 nodes of 4 heads a kv head are
-  // 4.25): eight waves of one tile share the work better than four of two (eight
-  // sequences of those over up to 17080 tokens 52.2 against 66.4 us, 128 prompt rows over
-  // 1155 tokens 24.0 against 26.0), which read LDS half as often in longer blocks
-  p.waves = p.rows == kFewRows ? kFewWaves : v_rows > 64 && v_rows <= 128 ? 8 : 4;
+  // blocks of 64 rows while all of them run at once (two a CU); where there are more,
+  // blocks of 128, which read LDS and L2 half as often: 2048 rows behind 2048 tokens
+  // in 1024 blocks of 64 69.9 us and in 512 of 128 56.7, 64 sequences of 17 rows of 4
+  // heads a kv head 135 and 103, but 777 rows of 4 heads a kv head in 392 of 64 20.5
+  // and in 200 of 128 (two splits) 35.9
+  const int64_t shorts = n_heads * seqs * ((v_rows + 63) / 64);
+  p.rows = !f16 || v_rows <= kFewRows ? kFewRows : v_rows <= 64 || shorts <= 512 ? 64 : 128;
   p.blocks = (int)((v_rows + p.rows - 1) / p.rows);
-  // a wave of few rows takes most of a SIMD's registers: one workgroup a CU
-  const int64_t target = p.rows == kFewRows ? 256 : 512, wgs = n_heads * seqs * p.blocks;
-  const int64_t least = p.rows == kFewRows ? kFewLeast : kRowsLeast;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, target / wgs, pages / least}));
+  const int64_t wgs = n_heads * seqs * p.blocks;
+  p.splits = 1;
+  if (p.rows == kFewRows) {
+    // a wave of few rows takes most of a SIMD's registers: one workgroup a CU.  Splits
+    // are worth their second launch where the blocks leave most of the chip idle and
+    // each still has some pages to walk: one row over 1028 tokens of 32 heads 15.1 us in
+    // one split, 10.8 + 3.6 in two, 8.4 + 3.0 in four
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, 256 / wgs, pages / kFewLeast}));
+    return p;
+  }
+  // the time of a step of four pages, of the second launch, and of a (row, head)'s state
+  // of a split written and read, in us: 300 rows of 32 heads over 700 tokens take 20.0
+  // us in one split and 23.9 in three, over 5000 tokens 121 and 55
+  constexpr double kStep = 1.1, kLaunch = 3.0, kState = 0.27e-3;
+  const int64_t steps = (pages + kRowsPages - 1) / kRowsPages;
+  const int64_t most = std::min<int64_t>({kMaxSplits, 512 / wgs, pages / kRowsLeast});
+  double best = kStep * (double)steps;
+  for (int64_t n = 2; n <= most; ++n) {
+    const double t = kStep * (double)((steps + n - 1) / n) + kLaunch + kState * (double)(n * v_rows * n_heads * seqs);
+    if (t >= best) continue;
+    best = t;
+    p.splits = (int)n;
+  }
   return p;
 }
 
@@ -928,13 +944,11 @@ static hipError_t launch_typed(const WindowArgs& a, float* ws, hipStream_t s) {
   if (p.rows == kFewRows) {
     TSS_LAUNCH((k_window_few<T, HD, WindowArgs>), grid, dim3(kFewWaves * 64), 0, s, a, p.splits, part_o, part_ml);
   } else if constexpr (sizeof(T) == 2) {
-    const dim3 block(p.waves * 64);
+    const dim3 block(kRowsPages * 64);
     if (p.rows == 64)
-      TSS_LAUNCH((k_window_rows<HD, 4, 1, WindowArgs>), grid, block, 0, s, a, p.splits, p.blocks, part_o, part_ml);
-    else if (p.waves == 8)
-      TSS_LAUNCH((k_window_rows<HD, 8, 1, WindowArgs>), grid, block, 0, s, a, p.splits, p.blocks, part_o, part_ml);
+      TSS_LAUNCH((k_window_rows<HD, 1, WindowArgs>), grid, block, 0, s, a, p.splits, p.blocks, part_o, part_ml);
     else
-      TSS_LAUNCH((k_window_rows<HD, 4, 2, WindowArgs>), grid, block, 0, s, a, p.splits, p.blocks, part_o, part_ml);
+      TSS_LAUNCH((k_window_rows<HD, 2, WindowArgs>), grid, block, 0, s, a, p.splits, p.blocks, part_o, part_ml);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
@@ -951,12 +965,12 @@ hipError_t launch_window(bool f16, int head_dim, const WindowArgs& a, void* work
 hipError_t launch_window_pass(int head_dim, const WindowPassArgs& a, hipStream_t s) {
   if (a.rows < 1 || a.rows > kPromptRows) return hipErrorInvalidValue;
   const int blocks = (a.rows + 127) / 128;  // passes take more than 64 rows
-  const dim3 grid(a.n_heads * blocks, 1, 1), block(4 * 64);
+  const dim3 grid(a.n_heads * blocks, 1, 1), block(kRowsPages * 64);
   float* none = nullptr;
   if (head_dim == 128)
-    TSS_LAUNCH((k_window_rows<128, 4, 2, WindowPassArgs>), grid, block, 0, s, a, 1, blocks, none, none);
+    TSS_LAUNCH((k_window_rows<128, 2, WindowPassArgs>), grid, block, 0, s, a, 1, blocks, none, none);
   else
-    TSS_LAUNCH((k_window_rows<64, 4, 2, WindowPassArgs>), grid, block, 0, s, a, 1, blocks, none, none);
+    TSS_LAUNCH((k_window_rows<64, 2, WindowPassArgs>), grid, block, 0, s, a, 1, blocks, none, none);
   return hipGetLastError();
 }
 
@@ -978,7 +992,7 @@ static hipError_t launch_step_typed(int n_items, const WindowStepArgs& a, float*
   if (p.rows == kFewRows)
     TSS_LAUNCH((k_window_few<T, HD, WindowStepArgs>), grid, dim3(kFewWaves * 64), 0, s, a, p.splits, part_o, part_ml);
   else if constexpr (sizeof(T) == 2)
-    TSS_LAUNCH((k_window_rows<HD, 4, 1, WindowStepArgs>), grid, dim3(4 * 64), 0, s, a, p.splits, p.blocks, part_o, part_ml);
+    TSS_LAUNCH((k_window_rows<HD, 1, WindowStepArgs>), grid, dim3(kRowsPages * 64), 0, s, a, p.splits, p.blocks, part_o, part_ml);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   // the timing of a launch is that of the one above
