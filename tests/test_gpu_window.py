@@ -124,6 +124,20 @@ def test_given_back_pages(kind):
     compare(out, q, rows, c, sinks, window)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("sinks,window", [(0, 0), (5, 100), (40, 64), (200, 1), (0, 333)])
+@pytest.mark.parametrize("group", [1, 3])
+def test_many_blocks(hd, sinks, window, group):
+    """More blocks of rows than run at once: longer blocks, ragged rows and lengths."""
+    rows = [300, 65, 1, 0, 129, 200, 77, 32]
+    c = Cache([411, 65, 700, 33, 129, 190, 500, 32], 16, hd, "f16", 58)
+    q = queries(rows, 16 * group, hd, "f16", 58)
+    out = ops.window_attention(q.to(DEV), c.pool, c.table, offsets(rows), c.lengths, sinks, window)
+    compare(out, q, rows, c, sinks, window)
+    again = ops.window_attention(q.to(DEV), c.pool, c.table, offsets(rows), c.lengths, sinks, window)
+    assert torch.equal(out, again)
+
+
 @pytest.mark.parametrize("kind", list(TYPES))
 @pytest.mark.parametrize("rows_each", [3, 100])
 def test_lost_page_hides_its_tokens(kind, rows_each):
