@@ -311,12 +311,14 @@ __global__ __launch_bounds__(W * 64, PARTS ? 6 : 1) void k_logprobs(LogprobArgs 
       if (k >= 0 && k < V) f(L::at(row, k), k);
     }
   };
-  // lane t of every wave has given token t and its logit
+  // lane t of every wave has given token t and its logit; a token outside the
+  // vocabulary is -1 from here on and is looked for nowhere
   int tok = -1;
   float xt = 0.f;
   if (lane < a.n_tokens) {
     tok = a.tokens[(size_t)r * a.n_tokens + lane];
-    if (tok >= 0 && tok < V) xt = L::at(row, tok);
+    if (tok < 0 || tok >= V) tok = -1;
+    if (tok >= 0) xt = L::at(row, tok);
   }
 
   float lm = x[0];
@@ -375,8 +377,8 @@ __global__ __launch_bounds__(W * 64, PARTS ? 6 : 1) void k_logprobs(LogprobArgs 
     int n = 0;
     const float y = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(xt), t));
     const int at = __builtin_amdgcn_readlane(tok, t);
-    if (wm < y && !odd) {
-      // nothing of this wave's comes before it
+    if (at < 0 || (wm < y && !odd)) {
+      // no such token (its rank is -1), or nothing of this wave's comes before it
     } else if (fabsf(y) < INFINITY && !odd) {
       // before the token an equal logit counts, behind it only a larger one:
       // at least y, or at least the float after it

@@ -195,3 +195,23 @@ def test_refusals():
                 lambda: ops.token_logprobs(x[:1].expand(4, 100)), lambda: ops.token_logprobs(x[:, :0])):
         with pytest.raises(ValueError):
             bad()
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("rows,vocab,pad,offset", [(2, 1000, 0, 0), (1, 1000, 3, 2), (3, 7000, 5, 3), (2, 50021, 1, 1)])
+def test_tokens_outside_the_vocabulary(kind, rows, vocab, pad, offset):
+    """Pads of any value, inside the last chunk's span too: NaN and -1, and nothing is read for them; the other tokens
+    of the row and the alternatives are as without them."""
+    x = logits(rows, vocab, kind, vocab, pad, offset)
+    pads = [vocab, vocab + 1, vocab + 3, vocab + 1051, 2 ** 31 - 1, -1, -2 ** 31]
+    g = torch.Generator().manual_seed(3)
+    for first in (0, 3):
+        tok = torch.randint(0, vocab, (rows, 8), generator=g, dtype=torch.int32)
+        for r in range(rows):
+            tok[r, 1:5] = torch.tensor([pads[(first + r + i) % 7] for i in range(4)], dtype=torch.int32)
+        tok = tok.to(DEV)
+        got = ops.token_logprobs(x, tok, 5)
+        check(x, tok, 5, got)
+        plain = ops.token_logprobs(x, tok[:, 5:].contiguous(), 5)
+        assert torch.equal(got.logprob[:, 5:], plain.logprob) and torch.equal(got.rank[:, 5:], plain.rank)
+        assert torch.equal(got.entropy, plain.entropy) and torch.equal(got.top_token, plain.top_token)
