@@ -40,6 +40,7 @@ constexpr int kLpVals = 32;       // logits a thread holds
 constexpr int kLpList = 512;      // candidates in LDS
 constexpr int kLpHolders = 256;   // threads that are looked through
 constexpr int kLpTokens = TSS_LOGPROBS_MAX_TOKENS;
+constexpr float kLpFar = 65536.f; // maxima beyond it take the logits' differences first
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 typedef unsigned long long u64;
@@ -335,7 +336,8 @@ __global__ __launch_bounds__(W * 64, PARTS ? 6 : 1) void k_logprobs(LogprobArgs 
   const float base = rs.base();
 
   // (x - m) log2 e as one fma: the rounding of m log2 e shifts all of them by
-  // the same `shift`, which is taken out of the sums again
+  // the same `shift`, which is taken out of the sums again (up to kLpFar it is at most
+  // 2^-8; the shift of a maximum of 1e10 would be hundreds of powers of two)
   const float b2 = base * kLog2e, shift = fmaf(base, kLog2e, -b2);
   float S = 0.f, T = 0.f;
 #pragma unroll
@@ -344,7 +346,7 @@ __global__ __launch_bounds__(W * 64, PARTS ? 6 : 1) void k_logprobs(LogprobArgs 
     S += e;
     T = fmaf(e, d, T);
   }
-  if (fabsf(base) > 1e30f) {  // m log2 e may overflow
+  if (fabsf(base) > kLpFar) {  // subtracted first, in two instructions a logit
     S = T = 0.f;
     const float base2 = again(base);
 #pragma unroll

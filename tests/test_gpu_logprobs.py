@@ -215,3 +215,29 @@ def test_tokens_outside_the_vocabulary(kind, rows, vocab, pad, offset):
         plain = ops.token_logprobs(x, tok[:, 5:].contiguous(), 5)
         assert torch.equal(got.logprob[:, 5:], plain.logprob) and torch.equal(got.rank[:, 5:], plain.rank)
         assert torch.equal(got.entropy, plain.entropy) and torch.equal(got.top_token, plain.top_token)
+
+
+@pytest.mark.parametrize("vocab", [40, 5000, 40000])
+@pytest.mark.parametrize("kind,size", [(k, s) for s in (1e4, 6e4, 1e5, 1e6, 1e9, 1e10, 1e12, 1e20, 1e30, 3e38)
+                                       for k, t in TYPES.items() if s <= torch.finfo(t).max])
+def test_rows_at_large_magnitudes(kind, vocab, size):
+    """Finite masks and maxima of any size: flat rows, masked rows, rows of which only the first tokens are left (whole
+    chunks at the mask's value), maxima far above zero, all of them spread that far."""
+    g = torch.Generator().manual_seed(vocab)
+    x = torch.randn(9, vocab, generator=g)
+    noise = x.clone()
+    x[0], x[1] = -size, size                           # flat
+    x[2, torch.rand(vocab, generator=g) < 0.9] = -size
+    x[3, 7:] = -size                                   # only the first are left
+    x[4, :vocab - 5] = -size                           # only the last are left
+    x[5] = size * (1 - 1e-3 * noise[5].abs().clamp_max(5))
+    x[6] = -size * (1 - 1e-3 * noise[6].abs().clamp_max(5))
+    x[7] = size * (noise[7] / 8).clamp(-1, 1)
+    x[8, vocab // 3] = size                            # one token far ahead
+    x = x.to(TYPES[kind]).to(DEV)
+    assert torch.isfinite(x).all()
+    tok = torch.randint(0, vocab, (9, 3), generator=g, dtype=torch.int32)
+    tok[:, 0] = torch.tensor([0, vocab - 1, 5, 3, vocab - 2, 1, 2, 4, vocab // 3])
+    tok = tok.to(DEV)
+    for top in (0, 9):
+        check(x, tok, top, ops.token_logprobs(x, tok, top))
