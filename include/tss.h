@@ -250,9 +250,10 @@ int tss_verify(tss_ctx* ctx, int32_t seq, const int32_t* draft_tokens, const int
  * contents: calls that overlap on one GPU (from several host threads, or on
  * streams that run at the same time) race, and the caller must serialise
  * them.  The merge counters are cleared at the start of every step.
- * tss_get_logits, tss_get_logits_device, tss_get_greedy and
- * tss_get_attn_split read the last step's workspace, so after a static call
- * they are valid only until the next call on that GPU reuses the scratch. */
+ * tss_get_logits, tss_get_logits_device, tss_get_greedy, tss_get_logprobs and
+ * tss_get_attn_split read the last step's workspace (and write nothing there),
+ * so after a static call they are valid only until the next call on that GPU
+ * reuses the scratch. */
 #define TSS_STATIC_SCRATCH_BYTES ((size_t)64 << 20)
 size_t tss_static_workspace_bytes(const tss_model_cfg* cfg);
 int tss_verify_static(tss_ctx* ctx, int32_t seq, const int32_t* draft_tokens, const int32_t* tree_parent,
@@ -368,9 +369,10 @@ int tss_seq_fork(tss_ctx* ctx, int32_t src, const int32_t* dst, int32_t n_dst, i
  * logits, to host memory; returns when they are there.  tokens: host,
  * [n_nodes][n_tokens], NULL for n_tokens = 0; a token outside the vocabulary gives
  * logprob NaN and rank -1.  Limits, results and their order as
- * tss_token_logprobs has them; outputs may be NULL.  TSS_EINVAL as for
- * tss_get_logits, TSS_ENOSPACE where the context's workspace is too small for
- * that many alternatives.  Paper: Algorithm 1 (the downstream metric of a task
+ * tss_token_logprobs has them; outputs may be NULL.  Its scratch is the part of
+ * the context's own workspace that the attention of a step uses.  TSS_EINVAL as
+ * for tss_get_logits, TSS_ENOSPACE where that part is too small for that many
+ * alternatives.  Paper: Algorithm 1 (the downstream metric of a task
  * whose answer is the most probable of several). */
 int tss_get_logprobs(tss_ctx* ctx, int32_t n_nodes, const int32_t* tokens, int32_t n_tokens, int32_t top_k,
                      float* logprob, int32_t* rank, float* entropy, float* top_logprob, int32_t* top_token);

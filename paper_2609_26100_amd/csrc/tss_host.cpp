@@ -1911,14 +1911,15 @@ int tss_get_logprobs(tss_ctx* c, int32_t n_nodes, const int32_t* tokens, int32_t
       top_k > TSS_LOGPROBS_MAX_TOP || top_k > V)
     return fail(c, TSS_EINVAL, "n_tokens outside [0, 8], top_k outside [0, min(32, vocab)] or no tokens");
   if (!launch_logprobs || !logprobs_fit(n_nodes, V)) return fail(c, TSS_EINVAL, "vocabulary too large");
-  // scratch: the attention's partial outputs, which nothing needs after the step:
-  // the given tokens, the results one behind the other, the call's own workspace
+  // scratch: the attention's partial outputs of the context's own workspace (also after
+  // a step in the static array, which other contexts use), which nothing needs after
+  // the step: the given tokens, the results one behind the other, the call's own workspace
   const size_t nt = (size_t)n_nodes * n_tokens, nk = (size_t)n_nodes * top_k;
   const size_t words = nt + 2 * nt + n_nodes + 2 * nk;
   const size_t own = align256(words * 4), need = own + logprobs_bytes(n_nodes, V, n_tokens, top_k);
-  if (need > c->out_wsl.part_slots * 64 * c->cfg.head_dim * 4)
+  if (need > c->wsl_own.part_slots * 64 * c->cfg.head_dim * 4)
     return fail(c, TSS_ENOSPACE, "the workspace has no room for that many alternatives");
-  uint8_t* base = const_cast<uint8_t*>(c->out_ws) + c->out_wsl.part_o;
+  uint8_t* base = c->ws_own + c->wsl_own.part_o;
   int32_t* dtok = (int32_t*)base;
   LogprobArgs a{};
   a.x = c->out_ws + c->out_wsl.logits;

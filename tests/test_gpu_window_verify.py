@@ -311,6 +311,21 @@ def test_logprobs_of_a_step(models, kind, nodes, n, top):
     np.testing.assert_array_equal(v.logits(nodes), lg)
 
 
+def test_logprobs_after_a_static_step_leave_its_scratch_alone(models):
+    """The library's static array is other contexts' too: what the call writes is in the context's own workspace."""
+    v, _ = models("bf16")
+    start(v, 0, synth.context_tokens(SMALL.vocab, 70, stream=173), 0, 0)
+    draft = synth.context_tokens(SMALL.vocab, 9, stream=174)
+    abi.tss_verify_static(v.ctx, 0, draft)
+    v.torch.cuda.synchronize()
+    before = v.workspace.clone()
+    got = v.logprobs(9, draft, 4)
+    changed = (v.workspace != before).sum().item()
+    # given tokens, log probabilities, ranks, entropies, alternatives: words that differ from what was there
+    assert changed > 9 * 8
+    check_logprobs(v.logits(9), draft, 4, got)
+
+
 def test_logprobs_refusals(models):
     v, _ = models("f32")
     start(v, 0, synth.context_tokens(TINY.vocab, 20, stream=172), 0, 0)
