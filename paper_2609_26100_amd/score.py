@@ -57,7 +57,7 @@ def continuation_logprobs(verifier, seq, root, continuations, scratch):
 
 def choose(verifier, seq, root, choices, scratch, per_token=False):
     """(index of the most probable choice, score of each): the sum of its tokens' log probabilities, or with per_token
-    their mean; the first of equal ones."""
+    their mean; the first of equal ones.  A score of NaN (from logits that are not finite) loses to every other."""
     lps = continuation_logprobs(verifier, seq, root, choices, scratch)
     scores = np.asarray([lp.mean(dtype=np.float64) if per_token else lp.sum(dtype=np.float64) for lp in lps])
-    return int(np.argmax(scores)), scores
+    return int(np.argmax(np.where(np.isnan(scores), -np.inf, scores))), scores

@@ -1,10 +1,11 @@
 """What the operators refuse, on the CPU: every check comes before any device work, so the addresses need not exist."""
 import ctypes
 
+import numpy as np
 import pytest
 import torch
 
-from paper_2609_26100_amd import ops
+from paper_2609_26100_amd import ops, score
 from paper_2609_26100_amd import tss as abi
 
 P = 0x10000  # a device address that no check touches
@@ -140,3 +141,10 @@ def test_message_names_the_last_refusal():
     with pytest.raises(abi.TSSError) as e:
         logprobs(top_k=40)
     assert abi.tss_last_error(None) in str(e.value) and "top_k" in abi.tss_last_error(None)
+
+
+def test_a_score_of_nan_is_not_chosen(monkeypatch):
+    scores = [[float("nan")], [-3.0, -1.0], [-2.0, -1.5], [float("nan"), 0.0]]
+    monkeypatch.setattr(score, "continuation_logprobs", lambda *a: [np.asarray(s, np.float32) for s in scores])
+    assert score.choose(None, 0, 1, scores, [1])[0] == 2
+    assert score.choose(None, 0, 1, scores, [1], per_token=True)[0] == 2
