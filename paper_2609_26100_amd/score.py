@@ -14,18 +14,26 @@ from __future__ import annotations
 import numpy as np
 
 
+def _tokens(c, vocab):
+    """A continuation as an int32 array; every token is checked here, for the last one never goes through the decoder."""
+    t = np.asarray(c)
+    if t.ndim != 1 or not len(t):
+        raise ValueError("a continuation is a list of at least one token")
+    if not ((t >= 0) & (t < vocab) & (t == np.floor(t))).all():
+        raise ValueError("a continuation holds a token outside the vocabulary")
+    return np.ascontiguousarray(t, dtype=np.int32)
+
+
 def continuation_logprobs(verifier, seq, root, continuations, scratch):
     """Log probabilities of each continuation's tokens, one float32 array a continuation.
 
     root: the last prompt token, whose K/V are not cached yet.  scratch: sequences of the verifier, other than seq,
     whose contents may be replaced; up to min(len(scratch), max_batch) continuations share a step.  Continuations longer
-    than a step's rows go through several steps."""
+    than a step's rows go through several steps.  A token outside the vocabulary is refused (ValueError)."""
     scratch = list(dict.fromkeys(int(s) for s in scratch))
     if not scratch or seq in scratch:
         raise ValueError("scoring needs scratch sequences other than the scored one")
-    conts = [np.ascontiguousarray(c, dtype=np.int32) for c in continuations]
-    if any(c.ndim != 1 or not len(c) for c in conts):
-        raise ValueError("a continuation is a list of at least one token")
+    conts = [_tokens(c, verifier.cfg.vocab) for c in continuations]
     out = [np.empty(len(c), np.float32) for c in conts]
     cfg = verifier.cfg
     rows = min(cfg.max_nodes * cfg.max_batch, 128 if verifier.shape.dtype == "bf16" else 64)

@@ -405,3 +405,14 @@ def test_scoring_refusals(models):
         kw = dict(dict(continuations=[[1, 2]], scratch=[1, 2]), **bad)
         with pytest.raises(ValueError):
             score.continuation_logprobs(v, 0, 1, kw["continuations"], kw["scratch"])
+
+
+def test_scoring_refuses_tokens_outside_the_vocabulary(models):
+    """The last token of a continuation never goes through the decoder: it is checked like the others."""
+    v, _ = models("f32")
+    start(v, 0, synth.context_tokens(TINY.vocab, 20, stream=195), 0, 0)
+    for bad in ([3, TINY.vocab], [TINY.vocab], [-1], [3, -1], [TINY.vocab, 3], [2 ** 32 + 3], [1.5]):
+        for fn in (score.continuation_logprobs, score.choose):
+            with pytest.raises(ValueError):
+                fn(v, 0, 1, [[4, 5], bad], [1, 2])
+    assert v.length(0) == 20
