@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 
 import numpy as np
 
@@ -136,6 +137,36 @@ def _ptr(a):
     return a.ctypes.data
 
 
+def _fit32(bits):
+    """Refuses whole numbers that 32 bits do not hold, given or-ed together: ctypes would cut the rest off.  (Beside a
+    negative one a longer one may pass, but the library refuses every negative one.)"""
+    if bits >> 31 not in (0, -1):
+        raise ValueError("a size, count or index is beyond 32 bits")
+
+
+def _int32s(a, name):
+    """A list or array of whole numbers as a contiguous int32 array; values that change in it are refused."""
+    try:
+        if isinstance(a, (list, tuple)):
+            try:
+                return np.asarray(array("i", a))
+            except TypeError:        # lists of lists, floats
+                pass
+        x = np.asarray(a)
+        if x.dtype != np.int32:
+            if x.dtype.kind in "iu":
+                y = x.astype(np.int32)
+            else:
+                with np.errstate(invalid="ignore"):
+                    y = x.astype(np.int32)
+            if not (x == y).all():
+                raise OverflowError
+            x = y
+    except OverflowError:
+        raise ValueError(f"{name} must be whole numbers of 32 bits") from None
+    return np.ascontiguousarray(x)
+
+
 def _check_op(status):
     if status != TSS_OK:
         raise TSSError(status, tss_last_error(None))
@@ -195,6 +226,7 @@ def tss_set_skip_mask(ctx, seq, mask):
 
 
 def tss_set_window(ctx, seq, sinks, window):
+    _fit32(seq | sinks | window)
     _check(lib().tss_set_window(ctx, seq, sinks, window), ctx, "tss_set_window")
 
 
@@ -332,14 +364,16 @@ def tss_seq_truncate(ctx, seq, n_kv):
 
 
 def tss_seq_fork(ctx, src, dst, n_kv):
-    d = np.ascontiguousarray(dst, dtype=np.int32)
+    _fit32(src | n_kv)
+    d = _int32s(dst, "dst")
     _check(lib().tss_seq_fork(ctx, src, _ptr(d), d.size, n_kv), ctx, "tss_seq_fork")
 
 
 def tss_get_logprobs(ctx, n_nodes, tokens=None, top_k=0):
     """Returns (logprob, rank, entropy, top_logprob, top_token) as numpy arrays: logprob and rank shaped as tokens
     ([n_nodes] or [n_nodes][n], None without), entropy [n_nodes], the top ones [n_nodes][top_k] (None for top_k = 0)."""
-    t = None if tokens is None else np.ascontiguousarray(tokens, dtype=np.int32)
+    _fit32(n_nodes | top_k)
+    t = None if tokens is None else _int32s(tokens, "tokens")
     if t is not None and (t.ndim not in (1, 2) or t.shape[0] != n_nodes):
         raise ValueError("tokens must be [n_nodes] or [n_nodes][n]")
     n = 0 if t is None else t.size // max(n_nodes, 1)
@@ -388,23 +422,27 @@ def tss_profile_read(ctx, reset=False):
 
 
 def tss_token_logprobs_bytes(rows, vocab, n_tokens, top_k) -> int:
+    _fit32(rows | vocab | n_tokens | top_k)
     return lib().tss_token_logprobs_bytes(rows, vocab, n_tokens, top_k)
 
 
 def tss_token_logprobs(hip_stream, logits, type, row_stride, rows, vocab, tokens, n_tokens, top_k, logprob, rank,
                        entropy, top_logprob, top_token, workspace, workspace_bytes):
     """Every tensor is a device address (or None)."""
+    _fit32(type | rows | vocab | n_tokens | top_k)
     _check_op(lib().tss_token_logprobs(hip_stream, logits, type, row_stride, rows, vocab, tokens, n_tokens, top_k,
                                        logprob, rank, entropy, top_logprob, top_token, workspace, workspace_bytes))
 
 
 def tss_window_attn_bytes(kv, n_q_heads, rows, max_rows, max_length, sinks, window) -> int:
+    _fit32(n_q_heads | rows | max_rows | max_length | sinks | window)
     return lib().tss_window_attn_bytes(kv, n_q_heads, rows, max_rows, max_length, sinks, window)
 
 
 def tss_window_attn(hip_stream, kv, layer, q, q_stride, n_q_heads, row_offsets, lengths, rows, max_rows, max_length,
                     sinks, window, scale, out, out_stride, workspace, workspace_bytes):
     """kv: a tss_paged_kv; every tensor is a device address (or None)."""
+    _fit32(layer | n_q_heads | rows | max_rows | max_length | sinks | window)
     _check_op(lib().tss_window_attn(hip_stream, kv, layer, q, q_stride, n_q_heads, row_offsets, lengths, rows,
                                     max_rows, max_length, sinks, window, scale, out, out_stride, workspace,
                                     workspace_bytes))
@@ -412,8 +450,7 @@ def tss_window_attn(hip_stream, kv, layer, q, q_stride, n_q_heads, row_offsets, 
 
 def tss_copy_pages(hip_stream, kv, src, dst):
     """kv: a tss_paged_kv; src and dst: host lists of page ids."""
-    s = np.ascontiguousarray(src, dtype=np.int32)
-    d = np.ascontiguousarray(dst, dtype=np.int32)
+    s, d = _int32s(src, "src"), _int32s(dst, "dst")
     if s.ndim != 1 or s.shape != d.shape:
         raise ValueError("src and dst must be lists of one length")
     _check_op(lib().tss_copy_pages(hip_stream, kv, _ptr(s), _ptr(d), len(s)))

@@ -69,7 +69,7 @@ class Verifier:
     def fork(self, src, dsts, n=None):
         """Makes the sequences dsts (one or several) forks of src: its first n tokens (all of them by default), mask
         and window."""
-        dsts = [int(x) for x in np.atleast_1d(np.asarray(dsts, dtype=np.int32))]
+        dsts = [int(x) for x in np.atleast_1d(abi._int32s(dsts, "dsts"))]
         abi.tss_seq_fork(self.ctx, src, dsts, self.length(src) if n is None else n)
         for x in dsts:
             self._mask[x] = self._mask[src].copy()

@@ -148,3 +148,45 @@ def test_a_score_of_nan_is_not_chosen(monkeypatch):
     monkeypatch.setattr(score, "continuation_logprobs", lambda *a: [np.asarray(s, np.float32) for s in scores])
     assert score.choose(None, 0, 1, scores, [1])[0] == 2
     assert score.choose(None, 0, 1, scores, [1], per_token=True)[0] == 2
+
+
+@pytest.mark.parametrize("far", [2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 63, -2 ** 31 - 1, -2 ** 32 + 5])
+def test_whole_numbers_beyond_32_bits_are_refused(far):
+    """None of them is cut off to another one on its way to the library."""
+    for name in ("type", "rows", "vocab", "n_tokens", "top_k"):
+        with pytest.raises(ValueError):
+            logprobs(**{name: far})
+    for name in ("layer", "n_q_heads", "rows", "max_rows", "max_length", "sinks", "window"):
+        with pytest.raises(ValueError):
+            window(**{name: far})
+    for i in range(4):
+        with pytest.raises(ValueError):
+            abi.tss_token_logprobs_bytes(*[far if j == i else 1 for j in range(4)])
+    for i in range(6):
+        with pytest.raises(ValueError):
+            abi.tss_window_attn_bytes(cache(), *[far if j == i else 4 for j in range(6)])
+    for call in (lambda: abi.tss_set_window(None, far, 0, 64), lambda: abi.tss_set_window(None, 0, far, 64),
+                 lambda: abi.tss_set_window(None, 0, 0, far), lambda: abi.tss_seq_fork(None, far, [1], 0),
+                 lambda: abi.tss_seq_fork(None, 0, [1], far), lambda: abi.tss_seq_fork(None, 0, [far], 0),
+                 lambda: abi.tss_get_logprobs(None, far), lambda: abi.tss_get_logprobs(None, 1, None, far),
+                 lambda: abi.tss_get_logprobs(None, 1, [far]), lambda: abi.tss_get_logprobs(None, 1, [[1, far]])):
+        with pytest.raises(ValueError):
+            call()
+
+
+@pytest.mark.parametrize("pages", [[2 ** 32 + 3], np.array([2 ** 32 + 3]), np.array([3 + 2 ** 32], np.uint64), [1.5],
+                                   np.array([1.5]), [float("nan")], [np.int64(2 ** 32 + 3)], [2 ** 70], (2 ** 31,)])
+def test_lists_whose_numbers_would_change_are_refused(pages):
+    for src, dst in ((pages, [2]), ([2], pages)):
+        with pytest.raises(ValueError):
+            abi.tss_copy_pages(None, cache(), src, dst)
+
+
+def test_lists_of_every_kind():
+    want = [1, 2, 1 << 30]
+    for a in (want, tuple(want), np.array(want), np.array(want, np.uint32), np.array(want, np.int32), np.array(want, float),
+              [float(x) for x in want], torch.tensor(want), np.array([want, want]).T[:, 0], [np.int64(x) for x in want]):
+        got = abi._int32s(a, "a")
+        assert got.dtype == np.int32 and got.tolist() == want and got.flags["C_CONTIGUOUS"]
+    assert abi._int32s([[1, 2], [3, 4]], "a").tolist() == [[1, 2], [3, 4]]
+    assert abi._int32s([], "a").size == 0 and abi._int32s(np.zeros(0), "a").size == 0
