@@ -27,6 +27,8 @@ from dataclasses import dataclass, field
 
 import numpy as np
 
+from . import tss as abi
+
 
 @dataclass
 class DecodeLogprobs:
@@ -40,6 +42,8 @@ class _Logprobs:
     """Collects the log probabilities of the emitted tokens, step by step."""
 
     def __init__(self, verifier, k):
+        if not 0 <= k <= min(abi.TSS_LOGPROBS_MAX_TOP, verifier.cfg.vocab):  # before the first step commits
+            raise ValueError("logprobs must be None or from 0 to min(32, vocab) alternatives")
         self.verifier, self.k, self.parts = verifier, k, []
 
     def add(self, n_nodes, nodes, emitted):

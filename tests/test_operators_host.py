@@ -1,11 +1,12 @@
 """What the operators refuse, on the CPU: every check comes before any device work, so the addresses need not exist."""
 import ctypes
+import types
 
 import numpy as np
 import pytest
 import torch
 
-from paper_2609_26100_amd import ops, score
+from paper_2609_26100_amd import decode, ops, score
 from paper_2609_26100_amd import tss as abi
 
 P = 0x10000  # a device address that no check touches
@@ -190,3 +191,33 @@ def test_lists_of_every_kind():
         assert got.dtype == np.int32 and got.tolist() == want and got.flags["C_CONTIGUOUS"]
     assert abi._int32s([[1, 2], [3, 4]], "a").tolist() == [[1, 2], [3, 4]]
     assert abi._int32s([], "a").size == 0 and abi._int32s(np.zeros(0), "a").size == 0
+
+
+class OneWayVerifier:
+    """Answers token 1 to everything and counts the steps that it commits."""
+
+    def __init__(self, vocab=100):
+        self.cfg, self.steps = types.SimpleNamespace(vocab=vocab), 0
+
+    def verify(self, seq, tokens, parent=None, mask=None, commit=False):
+        self.steps += commit
+        return 0, 1
+
+    def logprobs(self, n_nodes, tokens=None, top_k=0):
+        return (np.full(n_nodes, -1, np.float32), np.zeros(n_nodes, np.int32), np.zeros(n_nodes, np.float32),
+                np.zeros((n_nodes, top_k), np.float32) if top_k else None,
+                np.zeros((n_nodes, top_k), np.int32) if top_k else None)
+
+
+def decodes(v, max_new, logprobs):
+    yield lambda: decode.autoregressive_decode(v, 0, 3, max_new, logprobs=logprobs)
+    yield lambda: decode.speculative_decode(v, 0, 3, max_new, lambda root, pos: ([root, 5], None), logprobs=logprobs)
+
+
+@pytest.mark.parametrize("k,vocab", [(33, 100), (-1, 100), (5, 4)])
+def test_decoding_refuses_numbers_of_alternatives_before_a_step(k, vocab):
+    v = OneWayVerifier(vocab)
+    for run in decodes(v, 4, k):
+        with pytest.raises(ValueError):
+            run()
+    assert v.steps == 0
