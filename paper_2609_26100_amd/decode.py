@@ -55,6 +55,9 @@ class _Logprobs:
         self.parts.append((lp[nodes], ent[nodes], tl[nodes] if self.k else none, tt[nodes] if self.k else none))
 
     def result(self, n):
+        if not self.parts:
+            return DecodeLogprobs(np.empty(0, np.float32), np.empty(0, np.float32), np.empty((0, self.k), np.float32),
+                                  np.empty((0, self.k), np.int32))
         a, b, c, d = (np.concatenate(x)[:n] for x in zip(*self.parts))
         return DecodeLogprobs(a, b, c.astype(np.float32), d.astype(np.int32))
 
@@ -104,7 +107,7 @@ def speculative_decode(verifier, seq, root, max_new, drafter, mask=None, logprob
         acc.append(int(al))
         root = int(nt)
     return DecodeResult(np.asarray(out[:max_new], dtype=np.int32), len(acc), acc, time.perf_counter() - t0, t_draft,
-                        lps.result(max_new) if lps is not None and acc else None)
+                        lps.result(max_new) if lps is not None else None)
 
 
 def autoregressive_decode(verifier, seq, root, max_new, mask=None, logprobs=None):
@@ -121,4 +124,4 @@ def autoregressive_decode(verifier, seq, root, max_new, mask=None, logprobs=None
             lps.add(1, [0], [int(nt)])
         root = int(nt)
     return DecodeResult(np.asarray(out, dtype=np.int32), max_new, [0] * max_new, time.perf_counter() - t0,
-                        logprobs=lps.result(max_new) if lps is not None and out else None)
+                        logprobs=lps.result(max_new) if lps is not None else None)

@@ -221,3 +221,16 @@ def test_decoding_refuses_numbers_of_alternatives_before_a_step(k, vocab):
         with pytest.raises(ValueError):
             run()
     assert v.steps == 0
+
+
+@pytest.mark.parametrize("k", [0, 3])
+def test_decoding_no_token_with_log_probabilities(k):
+    for n in (0, 2):
+        for run in decodes(OneWayVerifier(), n, k):
+            r = run()
+            assert len(r.tokens) == n
+            assert [x.shape for x in (r.logprobs.logprob, r.logprobs.entropy, r.logprobs.top_logprob,
+                                      r.logprobs.top_token)] == [(n,), (n,), (n, k), (n, k)]
+            assert [x.dtype for x in (r.logprobs.logprob, r.logprobs.top_logprob, r.logprobs.top_token)] == [
+                np.float32, np.float32, np.int32]
+    assert all(run().logprobs is None for run in decodes(OneWayVerifier(), 0, None))
