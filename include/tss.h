@@ -489,7 +489,8 @@ typedef struct {
  *   q, out: [rows][n_q_heads][head_dim] of the cache's type, rows q_stride /
  *     out_stride elements apart (multiples of 8), aligned to 16 bytes; n_q_heads
  *     is a multiple of n_kv_heads, query head h reads kv head
- *     h / (n_q_heads / n_kv_heads).  out may be q.
+ *     h / (n_q_heads / n_kv_heads).  out may be q (with its stride), otherwise
+ *     they share no element.
  *   row_offsets [n_seqs + 1] (increasing from 0), lengths [n_seqs]: device.
  *   max_rows, max_length: upper bounds of a sequence's rows and length; rows
  *     beyond max_rows are not computed.  Lengths beyond the page table or

@@ -13,6 +13,7 @@ pack_pages and unpack_pages convert.
 """
 from __future__ import annotations
 
+import ctypes
 from typing import NamedTuple, Optional
 
 import torch
@@ -120,8 +121,9 @@ def window_attention(q, pages, page_table, row_offsets, lengths, sinks=0, window
     q: [rows][heads][head_dim] of the cache's type, heads a multiple of the cache's; page_table: int32
     [sequences][n]; row_offsets: int32 [sequences + 1], increasing from 0; lengths: int32 [sequences], cached
     tokens with the queries' own.  max_rows and max_length: upper bounds of a sequence's rows and length (without
-    them all of q's rows and the page table's tokens; tighter bounds launch less).  out: like q, may be q.  Rows of
-    out behind the last sequence are left as they were."""
+    them all of q's rows and the page table's tokens; tighter bounds launch less).  scale: factor of q k, above 0;
+    None for 1 / sqrt(head_dim).  out: like q, may be q, otherwise shares no element with it.  Rows of out behind the
+    last sequence are left as they were."""
     kv = _cache(pages, page_table)
     dev = pages.device
     _on_device(q, "q", dev)
@@ -144,7 +146,10 @@ def window_attention(q, pages, page_table, row_offsets, lengths, sinks=0, window
     max_rows = rows if max_rows is None else min(max_rows, rows)
     cap = kv.table_stride * PAGE
     max_length = cap if max_length is None else min(max_length, cap)
-    scale = 0.0 if scale is None else float(scale)
+    if scale is None:
+        scale = 0.0                      # the library's default
+    elif ctypes.c_float(scale).value == 0:
+        raise ValueError("scale must not be 0 in fp32 (None is 1 / sqrt(head_dim))")
     need = abi.tss_window_attn_bytes(kv, heads, rows, max_rows, max_length, sinks, window)
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     width = heads * hd

@@ -311,3 +311,12 @@ def test_refusals():
     with pytest.raises(ops.abi.TSSError):  # rows that are not aligned
         wide = torch.zeros(2, 300, dtype=torch.float16, device=DEV)
         call(q=wide[:, 4:260].unflatten(1, (4, 64)))
+
+
+def test_scale_of_zero_is_refused():
+    """None is 1 / sqrt(head_dim); a factor that is 0 in fp32 would be taken for it."""
+    c = Cache([40], 2, 64, "f16", 66)
+    q = queries([2], 4, 64, "f16", 66).to(DEV)
+    for scale in (0.0, -0.0, 1e-50):
+        with pytest.raises(ValueError):
+            ops.window_attention(q, c.pool, c.table, offsets([2]), c.lengths, scale=scale)
