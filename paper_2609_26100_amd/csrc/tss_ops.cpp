@@ -122,7 +122,11 @@ int tss_window_attn(void* hip_stream, const tss_paged_kv* kv, int32_t layer, con
   if (layer < 0 || layer >= kv->n_layers) return refuse(TSS_EINVAL, me, "no such layer");
   if (const char* f = window_fault(kv, n_q_heads, rows, max_rows, max_length, sinks, window))
     return refuse(TSS_EINVAL, me, f);
-  if (!(scale >= 0.f) || std::isinf(scale)) return refuse(TSS_EINVAL, me, "scale must be finite and not negative");
+  // in powers of two, as the kernels take it
+  const float scale_log2 =
+      (float)(1.4426950408889634 * (scale > 0.f ? (double)scale : 1.0 / std::sqrt((double)kv->head_dim)));
+  if (!(scale >= 0.f) || std::isinf(scale_log2))
+    return refuse(TSS_EINVAL, me, "scale must be finite (its product with log2 e too) and not negative");
   const int64_t width = (int64_t)n_q_heads * kv->head_dim;
   if (rows == 0 || max_rows == 0 || kv->n_seqs == 0) return TSS_OK;
   if (q_stride < width || out_stride < width || q_stride % 8 || out_stride % 8)
@@ -153,7 +157,7 @@ int tss_window_attn(void* hip_stream, const tss_paged_kv* kv, int32_t layer, con
   a.max_length = max_length;
   a.sinks = sinks;
   a.window = window;
-  a.scale_log2 = (float)(1.4426950408889634 * (scale > 0.f ? (double)scale : 1.0 / std::sqrt((double)kv->head_dim)));
+  a.scale_log2 = scale_log2;
   return launched(launch_window(kv->type == TSS_T_F16, kv->head_dim, a, workspace, (hipStream_t)hip_stream), me);
 }
 

@@ -234,3 +234,11 @@ def test_decoding_no_token_with_log_probabilities(k):
             assert [x.dtype for x in (r.logprobs.logprob, r.logprobs.top_logprob, r.logprobs.top_token)] == [
                 np.float32, np.float32, np.int32]
     assert all(run().logprobs is None for run in decodes(OneWayVerifier(), 0, None))
+
+
+def test_scale_whose_power_of_two_overflows_is_refused():
+    """A factor of finite scores that is finite itself, but not in powers of two."""
+    for scale in (2.4e38, 3.4e38):
+        with pytest.raises(abi.TSSError) as e:
+            window(scale=scale)
+        assert e.value.status == abi.TSS_EINVAL and "scale" in str(e.value)
