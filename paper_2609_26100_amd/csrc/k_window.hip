@@ -56,6 +56,11 @@ constexpr float kLowest = -3e38f;  // running maximum of a row that has seen not
 // those up to 1 (their rounding is relative), and almost no step has to rescale
 // its outputs, where with a threshold of 0 some row of sixteen nearly always rises.
 constexpr float kRise = 8.f;
+// A probability is 2^(S scale - m) in one fma, whose product is not rounded while m
+// was: up to kFar that makes a factor of at most 2^(2^-8) that the sums share, at 1e9 one
+// of up to 2^32, beyond fp16.  Where a reference maximum is farther from zero the
+// product is rounded first (2048 rows of 32 heads 0.4 us more for the test).
+constexpr float kFar = 65536.f;
 
 // Over the four lanes l, l ^ 16, l ^ 32, l ^ 48 of a row.
 __device__ __forceinline__ float max4(float x) {
@@ -69,6 +74,16 @@ __device__ __forceinline__ float sum4(float x) {
   x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
   const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(h[0]) + __uint_as_float(h[1]);
+}
+
+// S scale - m with the product rounded by itself (the empty asm keeps it out of an fma).
+__device__ __forceinline__ void round_exponents(f32x4& S, float scale, float m) {
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    float x = S[v] * scale;
+    asm volatile("" : "+v"(x));
+    S[v] = x - m;
+  }
 }
 
 // A block of virtual rows of one sequence and the pages it walks.
@@ -403,12 +418,21 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(A a, int split
     mx = max4(fmaxf(m, mx * a.scale_log2));
     const float alpha = __builtin_amdgcn_exp2f(m - mx);
     m = mx;
+    if (__any(fabsf(m) > kFar)) {
+#pragma unroll
+      for (int p = 0; p < PP; ++p) round_exponents(S[p], a.scale_log2, m);
+    } else {
+#pragma unroll
+      for (int p = 0; p < PP; ++p)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) S[p][v] = S[p][v] * a.scale_log2 - m;
+    }
     float sum = 0.f;
 #pragma unroll
     for (int p = 0; p < PP; ++p)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        S[p][v] = __builtin_amdgcn_exp2f(S[p][v] * a.scale_log2 - mx);
+        S[p][v] = __builtin_amdgcn_exp2f(S[p][v]);
         sum += S[p][v];
       }
     l = l * alpha + sum;
@@ -580,6 +604,7 @@ __global__ __launch_bounds__(kRowsPages * 64, 2) void k_window_rows(A a, int spl
   Row<A> row[TILES];
   f32x4 O[TILES][2 * NK];  // [2 i + j]: dims 32 i + 8 grp + 2 v + j
   float m_run[TILES], l_run[TILES];
+  float rise = kRise;  // scores beyond a reference by more raise it
 #pragma unroll
   for (int t = 0; t < TILES; ++t) {
     const int v = b.v0 + min(w0 + t * 16 + r16, b.n_v - 1);
@@ -656,19 +681,30 @@ __global__ __launch_bounds__(kRowsPages * 64, 2) void k_window_rows(A a, int spl
 #pragma unroll
         for (int v = 0; v < 4; ++v) mx = fmaxf(mx, S[t][p][v]);
       mx = max4(mx * a.scale_log2);
-      if (__any(mx > m_run[t] + kRise)) {
-        const float top = mx > m_run[t] + kRise ? mx : m_run[t];
-        const float alpha = __builtin_amdgcn_exp2f(m_run[t] - top);
-        m_run[t] = top;
+      float m = m_run[t];
+      if (__any(mx - m > rise)) {
+        m = mx - m <= kRise ? m : mx;
+        const float alpha = __builtin_amdgcn_exp2f(m_run[t] - m);
+        m_run[t] = m;
         l_run[t] *= alpha;
 #pragma unroll
         for (int n = 0; n < 2 * NK; ++n) O[t][n] *= alpha;
+        if (__any(fabsf(m) > kFar && m != kLowest)) {
+          // here in every step from now on: exponents first, in the scores' units and from 0
+#pragma unroll
+          for (int p = 0; p < kRowsPages; ++p) {
+            round_exponents(S[t][p], a.scale_log2, m);
+            S[t][p] *= 1.f / a.scale_log2;
+          }
+          m = 0.f;
+          rise = -INFINITY;
+        }
       }
 #pragma unroll
       for (int p = 0; p < kRowsPages; ++p)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const float e = __builtin_amdgcn_exp2f(S[t][p][v] * a.scale_log2 - m_run[t]);
+          const float e = __builtin_amdgcn_exp2f(S[t][p][v] * a.scale_log2 - m);
           l_run[t] += e;
           P[t][p >> 1][(p & 1) * 4 + v] = (_Float16)e;
         }

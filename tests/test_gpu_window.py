@@ -320,3 +320,25 @@ def test_scale_of_zero_is_refused():
     for scale in (0.0, -0.0, 1e-50):
         with pytest.raises(ValueError):
             ops.window_attention(q, c.pool, c.table, offsets([2]), c.lengths, scale=scale)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("rows", [1, 40, 200])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("size", [300.0, 3e3, 3e4])
+def test_scores_far_from_zero(kind, rows, sign, size):
+    """Equal scores of any finite size: the mean of V, as at zero.  Scores of up to 6e10 times 1 / 8."""
+    n, heads, hd = 250, 2, 64
+    c = Cache([n], heads, hd, kind, 67)
+    k, v = c.kv[0]
+    k[:] = sign * size
+    c.pool[0, c.table[0, :16].long()] = ops.pack_pages(k, v).to(DEV)
+    q = torch.full((rows, heads, hd), size, dtype=TYPES[kind])
+    got = ops.window_attention(q.to(DEV), c.pool, c.table, offsets([rows]), c.lengths, 0, 0).double().cpu()
+    half = ref.HALF if kind == "f16" else ref.F32
+    for r in range(rows):
+        seen = v[: n - rows + r + 1].double()
+        want = seen.mean(0)
+        # equal weights (powers of two, exact), sums of n terms in fp32 and the roundings of 1 / L and of the result
+        bound = n * ref.F32 * seen.abs().mean(0) * 2 + (half + 2 * ref.F32) * want.abs() + 2.0 ** -25
+        assert ((got[r] - want).abs() <= bound).all(), (r, float((got[r] - want).abs().max()))
