@@ -56,6 +56,13 @@ constexpr float kLowest = -3e38f;  // running maximum of a row that has seen not
 // those up to 1 (their rounding is relative), and almost no step has to rescale
 // its outputs, where with a threshold of 0 some row of sixteen nearly always rises.
 constexpr float kRise = 8.f;
+// Probabilities that go to fp16 are relative to a reference this many powers of two
+// below the maximum, so that the largest is 2^15 in the kernel of few rows and, with
+// kRise, 2^7 to 2^15 in that of many.  A small one's rounding is then at most 2^-40 or
+// 2^-32 of the largest; with the maximum as the reference it would be 2^-25, and 20000
+// tokens of 2^-26 each, 3e-4 of a row's weight together, would come to nothing.  The
+// sums have the same factor, so it cancels.
+constexpr float kFewDown = 15.f, kRowsDown = 7.f;
 // A probability is 2^(S scale - m) in one fma, whose product is not rounded while m
 // was: up to kFar that makes a factor of at most 2^(2^-8) that the sums share, at 1e9 one
 // of up to 2^32, beyond fp16.  Where a reference maximum is farther from zero the
@@ -415,7 +422,9 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(A a, int split
     for (int p = 0; p < PP; ++p)
 #pragma unroll
       for (int v = 0; v < 4; ++v) mx = fmaxf(mx, S[p][v]);
-    mx = max4(fmaxf(m, mx * a.scale_log2));
+    mx *= a.scale_log2;
+    if constexpr (sizeof(T) == 2) mx -= fabsf(mx) > kFar ? 0.f : kFewDown;
+    mx = max4(fmaxf(m, mx));
     const float alpha = __builtin_amdgcn_exp2f(m - mx);
     m = mx;
     if (__any(fabsf(m) > kFar)) {
@@ -604,7 +613,7 @@ __global__ __launch_bounds__(kRowsPages * 64, 2) void k_window_rows(A a, int spl
   Row<A> row[TILES];
   f32x4 O[TILES][2 * NK];  // [2 i + j]: dims 32 i + 8 grp + 2 v + j
   float m_run[TILES], l_run[TILES];
-  float rise = kRise;  // scores beyond a reference by more raise it
+  float rise = kRise + kRowsDown;  // scores beyond a reference by more raise it
 #pragma unroll
   for (int t = 0; t < TILES; ++t) {
     const int v = b.v0 + min(w0 + t * 16 + r16, b.n_v - 1);
@@ -683,7 +692,7 @@ __global__ __launch_bounds__(kRowsPages * 64, 2) void k_window_rows(A a, int spl
       mx = max4(mx * a.scale_log2);
       float m = m_run[t];
       if (__any(mx - m > rise)) {
-        m = mx - m <= kRise ? m : mx;
+        m = mx - m <= kRise + kRowsDown ? m : fabsf(mx) > kFar ? mx : mx - kRowsDown;
         const float alpha = __builtin_amdgcn_exp2f(m_run[t] - m);
         m_run[t] = m;
         l_run[t] *= alpha;

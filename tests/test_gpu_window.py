@@ -342,3 +342,37 @@ def test_scores_far_from_zero(kind, rows, sign, size):
         # equal weights (powers of two, exact), sums of n terms in fp32 and the roundings of 1 / L and of the result
         bound = n * ref.F32 * seen.abs().mean(0) * 2 + (half + 2 * ref.F32) * want.abs() + 2.0 ** -25
         assert ((got[r] - want).abs() <= bound).all(), (r, float((got[r] - want).abs().max()))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("rows", [1, 260])
+def test_many_small_weights_beside_a_dominant_one(rows, hd):
+    """A sink with nearly all of the weight and 20000 tokens of e^-18 of it each: together 3e-4, no less than they are.
+    No splits: one workgroup walks all of a row's pages."""
+    n, heads, seqs = 20000, 64, 4 if rows == 1 else 1
+    g = torch.Generator().manual_seed(hd)
+    k, v = torch.zeros(n, heads, hd), 4 + torch.randn(n, heads, hd, generator=g)
+    k[0, :, 0] = 18.0
+    v[0] = 0
+    k, v = k.half(), v.half()
+    pages = ops.pack_pages(k, v)[None].to(DEV)
+    table = torch.arange(pages.shape[1], dtype=torch.int32, device=DEV).repeat(seqs, 1)
+    q = torch.zeros(seqs * rows, heads, hd)
+    q[:, :, 0] = hd ** 0.5
+    lens = torch.full((seqs,), n, dtype=torch.int32, device=DEV)
+    q = q.half()
+    assert ops.abi.tss_window_attn_bytes(ops._cache(pages, table), heads, seqs * rows, rows, n, 0, 0) == 0
+    got = ops.window_attention(q.to(DEV), pages, table, offsets([rows] * seqs), lens, max_rows=rows).double().cpu()
+    for r, h in ((0, 0), (seqs * rows - 1, heads - 1), (rows // 2, 5)):
+        see = torch.arange(n) <= (n - rows + r % rows)
+        s = (q[r, h].double() @ k[:, h].double().T / hd ** 0.5).masked_fill(~see, -torch.inf)
+        p = torch.softmax(s, 0)
+        want = p @ v[:, h].double()
+        # as ref.attention bounds it, but a weight's rounding in fp16 is at most 2^-32 of the largest: the scores are
+        # exact (one product of two fp16 values and a power of two or 1/sqrt(128)), 18 log2 e and its exponent round
+        pv, big = p @ v[:, h].double().abs(), float(v[:, h].abs().max())
+        bound = 2 * (18 + 8) * 6 * ref.F32 * pv + 2 * n * ref.F32 * pv + ref.HALF * pv + n * 2.0 ** -32 * big \
+            + ref.HALF * want.abs() + 2.0 ** -25
+        err = (got[r, h] - want).abs()
+        print(f"{rows} rows of {hd}: {float(err.max()):.3g}, bound {float(bound.min()):.3g}, output {float(want.min()):.3g}")
+        assert (err <= bound).all()
