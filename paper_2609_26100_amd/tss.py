@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from array import array
 
 import numpy as np
@@ -137,11 +138,15 @@ def _ptr(a):
     return a.ctypes.data
 
 
-def _fit32(bits):
-    """Refuses whole numbers that 32 bits do not hold, given or-ed together: ctypes would cut the rest off.  (Beside a
-    negative one a longer one may pass, but the library refuses every negative one.)"""
-    if bits >> 31 not in (0, -1):
-        raise ValueError("a size, count or index is beyond 32 bits")
+_PACK = [struct.Struct(f"{n}i").pack for n in range(8)]
+
+
+def _fit32(*numbers):
+    """Refuses what is no whole number of 32 bits: ctypes would cut the rest off."""
+    try:
+        _PACK[len(numbers)](*numbers)
+    except struct.error:
+        raise ValueError("a size, count or index is no whole number of 32 bits") from None
 
 
 def _int32s(a, name):
@@ -226,7 +231,7 @@ def tss_set_skip_mask(ctx, seq, mask):
 
 
 def tss_set_window(ctx, seq, sinks, window):
-    _fit32(seq | sinks | window)
+    _fit32(seq, sinks, window)
     _check(lib().tss_set_window(ctx, seq, sinks, window), ctx, "tss_set_window")
 
 
@@ -364,7 +369,7 @@ def tss_seq_truncate(ctx, seq, n_kv):
 
 
 def tss_seq_fork(ctx, src, dst, n_kv):
-    _fit32(src | n_kv)
+    _fit32(src, n_kv)
     d = _int32s(dst, "dst")
     _check(lib().tss_seq_fork(ctx, src, _ptr(d), d.size, n_kv), ctx, "tss_seq_fork")
 
@@ -372,7 +377,7 @@ def tss_seq_fork(ctx, src, dst, n_kv):
 def tss_get_logprobs(ctx, n_nodes, tokens=None, top_k=0):
     """Returns (logprob, rank, entropy, top_logprob, top_token) as numpy arrays: logprob and rank shaped as tokens
     ([n_nodes] or [n_nodes][n], None without), entropy [n_nodes], the top ones [n_nodes][top_k] (None for top_k = 0)."""
-    _fit32(n_nodes | top_k)
+    _fit32(n_nodes, top_k)
     t = None if tokens is None else _int32s(tokens, "tokens")
     if t is not None and (t.ndim not in (1, 2) or t.shape[0] != n_nodes):
         raise ValueError("tokens must be [n_nodes] or [n_nodes][n]")
@@ -422,27 +427,27 @@ def tss_profile_read(ctx, reset=False):
 
 
 def tss_token_logprobs_bytes(rows, vocab, n_tokens, top_k) -> int:
-    _fit32(rows | vocab | n_tokens | top_k)
+    _fit32(rows, vocab, n_tokens, top_k)
     return lib().tss_token_logprobs_bytes(rows, vocab, n_tokens, top_k)
 
 
 def tss_token_logprobs(hip_stream, logits, type, row_stride, rows, vocab, tokens, n_tokens, top_k, logprob, rank,
                        entropy, top_logprob, top_token, workspace, workspace_bytes):
     """Every tensor is a device address (or None)."""
-    _fit32(type | rows | vocab | n_tokens | top_k)
+    _fit32(type, rows, vocab, n_tokens, top_k)
     _check_op(lib().tss_token_logprobs(hip_stream, logits, type, row_stride, rows, vocab, tokens, n_tokens, top_k,
                                        logprob, rank, entropy, top_logprob, top_token, workspace, workspace_bytes))
 
 
 def tss_window_attn_bytes(kv, n_q_heads, rows, max_rows, max_length, sinks, window) -> int:
-    _fit32(n_q_heads | rows | max_rows | max_length | sinks | window)
+    _fit32(n_q_heads, rows, max_rows, max_length, sinks, window)
     return lib().tss_window_attn_bytes(kv, n_q_heads, rows, max_rows, max_length, sinks, window)
 
 
 def tss_window_attn(hip_stream, kv, layer, q, q_stride, n_q_heads, row_offsets, lengths, rows, max_rows, max_length,
                     sinks, window, scale, out, out_stride, workspace, workspace_bytes):
     """kv: a tss_paged_kv; every tensor is a device address (or None)."""
-    _fit32(layer | n_q_heads | rows | max_rows | max_length | sinks | window)
+    _fit32(layer, n_q_heads, rows, max_rows, max_length, sinks, window)
     _check_op(lib().tss_window_attn(hip_stream, kv, layer, q, q_stride, n_q_heads, row_offsets, lengths, rows,
                                     max_rows, max_length, sinks, window, scale, out, out_stride, workspace,
                                     workspace_bytes))

@@ -242,3 +242,13 @@ def test_scale_whose_power_of_two_overflows_is_refused():
         with pytest.raises(abi.TSSError) as e:
             window(scale=scale)
         assert e.value.status == abi.TSS_EINVAL and "scale" in str(e.value)
+
+
+def test_sizes_of_every_whole_type():
+    """A short type beside a longer number is no reason to refuse, a fraction is one."""
+    for t in (int, np.uint8, np.int16, np.int64, np.uint64):
+        assert abi.tss_token_logprobs_bytes(t(3), 40000, t(1), t(5)) == abi.tss_token_logprobs_bytes(3, 40000, 1, 5) > 0
+        assert abi.tss_window_attn_bytes(cache(), t(8), t(4), t(4), 1024, t(4), t(100)) == 0
+    for bad in (1.0, np.float32(2), None, "4"):
+        with pytest.raises(ValueError):
+            abi.tss_token_logprobs_bytes(bad, 40000, 1, 5)
