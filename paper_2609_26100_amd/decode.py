@@ -42,9 +42,9 @@ class _Logprobs:
     """Collects the log probabilities of the emitted tokens, step by step."""
 
     def __init__(self, verifier, k):
-        if not 0 <= k <= min(abi.TSS_LOGPROBS_MAX_TOP, verifier.cfg.vocab):  # before the first step commits
+        if k not in range(min(abi.TSS_LOGPROBS_MAX_TOP, verifier.cfg.vocab) + 1):  # before the first step commits
             raise ValueError("logprobs must be None or from 0 to min(32, vocab) alternatives")
-        self.verifier, self.k, self.parts = verifier, k, []
+        self.verifier, self.k, self.parts = verifier, int(k), []
 
     def add(self, n_nodes, nodes, emitted):
         """`emitted` follow `nodes` of the last verify, which had n_nodes."""

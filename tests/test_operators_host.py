@@ -252,3 +252,13 @@ def test_sizes_of_every_whole_type():
     for bad in (1.0, np.float32(2), None, "4"):
         with pytest.raises(ValueError):
             abi.tss_token_logprobs_bytes(bad, 40000, 1, 5)
+
+
+@pytest.mark.parametrize("k", [1.5, float("nan"), "3"])
+def test_decoding_refuses_what_is_no_number_of_alternatives(k):
+    v = OneWayVerifier()
+    for run in decodes(v, 4, k):
+        with pytest.raises(ValueError):
+            run()
+    assert v.steps == 0
+    assert decode.autoregressive_decode(v, 0, 3, 2, logprobs=2.0).logprobs.top_token.shape == (2, 2)
