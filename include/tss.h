@@ -196,7 +196,9 @@ int tss_set_skip_mask(tss_ctx* ctx, int32_t seq, const uint8_t* mask);
  * Attention then reads the pages of the sinks and the window instead of the
  * whole context, in prefill, verify, batches and sweeps.  Positions and the
  * sequence's capacity are as without a window, and tokens that are not seen stay
- * in the cache (a wider window set later sees them again).  TSS_EINVAL for an
+ * in the cache (a wider window set later sees them again).  The other sequences
+ * of a step that has one with a window go through the same kernels: their
+ * results are those of a step without up to the order of sums.  TSS_EINVAL for an
  * unknown sequence, negative sinks or another window.  Paper: Problem
  * Formulation (verification against the cached prefix, here a part of it). */
 int tss_set_window(tss_ctx* ctx, int32_t seq, int32_t sinks, int32_t window);
