@@ -55,10 +55,10 @@ constexpr int kMaxSplits = 64;
 // of eight waves for that of few.
 constexpr int kFewLeast = 16, kRowsLeast = 8;
 constexpr float kLowest = -3e38f;  // running maximum of a row that has seen nothing
-// A row's reference maximum is raised where the scores exceed it by this (in
-// powers of two): probabilities up to 2^8 of the largest fit fp16 as well as
-// those up to 1 (their rounding is relative), and almost no step has to rescale
-// its outputs, where with a threshold of 0 some row of sixteen nearly always rises.
+// A row's reference is raised where a score exceeds the maximum that set it by this
+// (in powers of two): larger probabilities fit fp16 as well (their rounding is
+// relative), and almost no step has to rescale its outputs, where with a threshold of
+// 0 some row of sixteen nearly always rises.
 constexpr float kRise = 8.f;
 // Probabilities that go to fp16 are relative to a reference this many powers of two
 // below the maximum, so that the largest is 2^15 in the kernel of few rows and, with
