@@ -521,6 +521,96 @@ int tss_window_attn(void* hip_stream, const tss_paged_kv* kv, int32_t layer, con
  * Problem Formulation (the cached prefix that several continuations share). */
 int tss_copy_pages(void* hip_stream, const tss_paged_kv* kv, const int32_t* src, const int32_t* dst, int32_t n);
 
+/* Appends rows to one layer of the cache, rotated to their positions: row i of a
+ * sequence of r rows (rows and lengths as tss_window_attn has them, so lengths
+ * count the new rows) is the token of slot p = lengths[s] - r + i.  Its K goes
+ * rotated and its V as it is to that slot, its queries rotated to q_out, ready
+ * for tss_window_attn or tss_prefix_attn.
+ *   q [rows][n_q_heads][head_dim], k, v [rows][n_kv_heads][head_dim] of `type`,
+ *     rows their stride apart (elements, multiples of 8: parts of one projection's
+ *     output, for instance), aligned to 16 bytes.  n_q_heads is any number; 0 with
+ *     q NULL appends alone.
+ *   positions: device [rows], the rotary position of each row (a tree's nodes); NULL:
+ *     its slot.  Any int32 is one.
+ *   inv_freq: host, head_dim / 2 frequencies f_j: dimensions j and j + head_dim / 2
+ *     turn by position * f_j, base^(-2j / head_dim) for LLaMA; NULL: no rotation.
+ *     They must be finite.  Angles are formed in 64 bits.
+ *   q_out: [rows][n_q_heads][head_dim] of the cache's type; may be q (of that type, with
+ *     its stride), otherwise it shares no element with an input.
+ *   max_rows: upper bound of a sequence's rows; rows beyond it are not taken.
+ * Everything is rounded once, to the cache's type (fp16: beyond 65504 to
+ * infinity).  Not written: rows behind the last sequence or before token 0 (more
+ * rows than tokens), and K and V of slots behind the page table or on pages outside
+ * the pool.  Slots of one call must be different ones.  Paper: Problem
+ * Formulation (the committed prefix grows by the accepted tokens). */
+int tss_append_kv(void* hip_stream, const tss_paged_kv* kv, int32_t layer, const void* q, int64_t q_stride,
+                  int32_t n_q_heads, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t type,
+                  const int32_t* row_offsets, const int32_t* lengths, const int32_t* positions, int32_t rows,
+                  int32_t max_rows, const double* inv_freq, void* q_out, int64_t q_out_stride);
+
+/* Attention of one layer for sequences that share a prefix: as tss_window_attn with
+ * window 0, but the pages that a group of sequences has in common are read once for
+ * all rows of the group.  Group g are the sequences group_offsets[g] ..
+ * group_offsets[g + 1] - 1, and the first shared[g] entries of their page tables
+ * name the same pages (the group's first sequence's are read).  Where a row of a
+ * group stands inside the shared pages, the group's pages from there on are read
+ * through each sequence's own table.
+ *   group_offsets [n_groups + 1] (increasing), shared [n_groups]: device.  Sequences
+ *     outside every group share nothing.  n_groups = 0: no group; group_offsets NULL
+ *     with n_groups 1: every sequence.
+ *   max_group_rows, max_shared: upper bounds of a group's rows and shared pages; what
+ *     a group shares beyond max_shared is read through the own tables, and a group of
+ *     more rows than max_group_rows shares nothing.
+ * All else as tss_window_attn: q, out, row_offsets, lengths, max_rows, max_length,
+ * scale, rows that see nothing, the cache's contents, and the workspace, of
+ * tss_prefix_attn_bytes() bytes.  Paper: Problem Formulation (several continuations of
+ * one cached prefix). */
+size_t tss_prefix_attn_bytes(const tss_paged_kv* kv, int32_t n_q_heads, int32_t rows, int32_t max_rows,
+                             int32_t max_length, int32_t n_groups, int32_t max_group_rows, int32_t max_shared);
+int tss_prefix_attn(void* hip_stream, const tss_paged_kv* kv, int32_t layer, const void* q, int64_t q_stride,
+                    int32_t n_q_heads, const int32_t* row_offsets, const int32_t* lengths, int32_t rows,
+                    int32_t max_rows, int32_t max_length, const int32_t* group_offsets, const int32_t* shared,
+                    int32_t n_groups, int32_t max_group_rows, int32_t max_shared, float scale, void* out,
+                    int64_t out_stride, void* workspace, size_t workspace_bytes);
+
+#define TSS_BEAMS_MAX 32
+#define TSS_BEAMS_MAX_N 64
+
+/* The n best continuations of each group of beams.  Beam b of group g has row
+ * g * n_beams + b of logits and of scores (the sum of its tokens' log probabilities);
+ * a candidate (b, t) is worth scores[b] + x[b][t] - ln sum e^x[b].  Candidates are
+ * ordered by that value, larger first, then by b, then by t.
+ *   logits: as tss_token_logprobs has them, [n_groups * n_beams][vocab].
+ *   scores: [n_groups * n_beams].  ended: like scores, or NULL: a beam whose entry is
+ *     not 0 has ended, and its one candidate is end_token (0 <= end_token < vocab), worth
+ *     scores[b].
+ *   score, parent, token: [n_groups][n], the values rounded to fp32, b and t.
+ * 1 <= n_beams <= 32, 1 <= n <= min(64, n_beams * vocab).  Values are held and compared
+ * in 64 bits, of sums of exponentials taken in 32.  Pairs that are no candidate are worth -inf:
+ * logits of -inf, all but the end_token of an ended beam, and every pair of a beam
+ * whose score is not finite or, if it has not ended, whose logits hold NaN or +inf or
+ * nothing but -inf; they come last, as b and t order them.
+ *   workspace: tss_beam_select_bytes() bytes, aligned to 16.
+ * n_groups = 0 launches nothing.  Paper: Table 3 and Algorithm 1 compare configurations
+ * by a task's metric, for which continuations are searched. */
+size_t tss_beam_select_bytes(int32_t n_groups, int32_t n_beams, int32_t vocab, int32_t n);
+int tss_beam_select(void* hip_stream, const void* logits, int32_t type, int64_t row_stride, int32_t n_groups,
+                    int32_t n_beams, int32_t vocab, const float* scores, const int32_t* ended, int32_t end_token,
+                    int32_t n, float* score, int32_t* parent, int32_t* token, void* workspace, size_t workspace_bytes);
+
+/* Reorders the cached tokens of beams, in every layer and in place: sequence
+ * g * n_beams + b of the page table becomes what sequence g * n_beams +
+ * parents[g * n_beams + b] was, all of a group at once (any map, exchanges too).
+ * Moved are pages from shared[g] on (NULL: 0), as many as hold the parent's
+ * lengths[] tokens, at most those of max_own tokens; a beam that is its own parent,
+ * or whose parent is outside [0, n_beams), stays.  kv->n_seqs must be a multiple of
+ * n_beams, 1 <= n_beams <= 32; parents, lengths [n_seqs], shared [n_seqs / n_beams]:
+ * device.  The moved pages must be each sequence's own; pages outside the
+ * pool are neither read nor written.  The caller moves its own lengths.  Paper:
+ * Problem Formulation (the committed prefix). */
+int tss_reorder_pages(void* hip_stream, const tss_paged_kv* kv, const int32_t* parents, int32_t n_beams,
+                      const int32_t* lengths, const int32_t* shared, int32_t max_own);
+
 /* Message of the context's last failure; with ctx = NULL, of the calling
  * thread's last failed tss_create or operator call. */
 const char* tss_last_error(const tss_ctx* ctx);

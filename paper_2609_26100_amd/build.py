@@ -19,7 +19,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libtss.so")
 SOURCES = ["tss_host.cpp", "tss_static.hip", "k_gemm.hip", "k_tile.hip", "k_attn.hip", "k_prompt.hip", "k_misc.hip",
-           "tss_ops.cpp", "k_logprob.hip", "k_window.hip", "k_pages.hip"]
+           "tss_ops.cpp", "k_logprob.hip", "k_window.hip", "k_pages.hip", "k_append.hip", "k_prefix.hip", "k_beams.hip"]
 
 
 def _hipcc():

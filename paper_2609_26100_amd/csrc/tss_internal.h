@@ -494,6 +494,53 @@ struct CopyArgs {
 };
 TSS_WEAK hipError_t launch_copy_pages(const CopyArgs& a, hipStream_t s);
 
+struct AppendArgs {
+  const void *q, *k, *v;   // rows q_stride, .. elements apart
+  void* q_out;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;
+  uint8_t* kv_pages;       // the layer's pages
+  const int32_t *page_table, *row_offsets, *lengths, *positions;
+  int n_pages, n_heads, n_q_heads, n_seqs, table_stride, rows, max_rows;
+  int type;                // of q, k, v: enum tss_tensor_type
+  int rotate;
+  double turns[64];        // inv_freq / (2 pi)
+};
+bool append_fits(int n_q_heads, int n_heads, int n_seqs, int max_rows);
+hipError_t launch_append(bool f16, int head_dim, const AppendArgs& a, hipStream_t s);
+
+struct PrefixArgs : WindowArgs {
+  const int32_t *group_offsets, *shared;
+  int n_groups, max_group_rows, max_shared;
+};
+bool prefix_fits(int n_heads, int group, int n_seqs, int max_rows, int n_groups, int max_group_rows);
+size_t prefix_bytes(bool f16, int head_dim, int n_heads, int group, int n_seqs, int rows, int max_rows, int max_length,
+                    int n_groups, int max_group_rows, int max_shared);
+hipError_t launch_prefix(bool f16, int head_dim, const PrefixArgs& a, void* workspace, hipStream_t s);
+
+struct BeamArgs {
+  const void* x;           // [n_groups * n_beams][vocab], rows `stride` elements apart
+  int64_t stride;
+  int n_groups, n_beams, vocab, type;
+  const float* scores;
+  const int32_t* ended;    // null: none has
+  int end_token, n;
+  float* score;            // [n_groups][n]
+  int32_t *parent, *token;
+};
+TSS_WEAK bool beams_fit(int n_groups, int n_beams, int vocab);
+TSS_WEAK size_t beams_bytes(int n_groups, int n_beams, int vocab, int n);
+TSS_WEAK hipError_t launch_beams(const BeamArgs& a, void* workspace, hipStream_t s);
+
+struct ReorderArgs {
+  uint8_t* pages;
+  size_t page_bytes, layer_bytes;
+  uint64_t layers[kMaxLayers / 64];  // bit l: layer l takes part
+  const int32_t *page_table, *parents, *lengths, *shared;
+  int n_layers, n_pages, n_groups, n_beams, table_stride, max_own;
+};
+TSS_WEAK bool reorder_fits(const ReorderArgs& a);
+TSS_WEAK hipError_t launch_reorder(const ReorderArgs& a, hipStream_t s);
+
 // Message of the calling thread's last failure outside a context
 // (tss_last_error(NULL)).
 void set_thread_error(const char* msg);

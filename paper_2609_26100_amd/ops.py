@@ -1,6 +1,8 @@
 """The operators of libtss.so on torch tensors: log probabilities of given
-tokens, attention with a sliding window and sinks over a paged KV cache, and
-copies of cache pages.
+tokens, attention with a sliding window and sinks over a paged KV cache, copies of
+cache pages; and those of decoding several continuations of one prompt: rows appended
+to the cache with the rotation of their positions, attention behind a shared prefix,
+the choice of the next beams and the reordering of their cached tokens.
 
 PyTorch only provides the device memory (outputs and workspaces) and the current
 stream of the tensors' device, on which every call is enqueued; no call waits.
@@ -14,6 +16,7 @@ pack_pages and unpack_pages convert.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import NamedTuple, Optional
 
 import torch
@@ -30,6 +33,12 @@ class TokenLogprobs(NamedTuple):
     entropy: torch.Tensor                # [rows], nats
     top_logprob: Optional[torch.Tensor]  # [rows][top_k], None for top_k = 0
     top_token: Optional[torch.Tensor]
+
+
+class BeamSelection(NamedTuple):
+    score: torch.Tensor                  # [groups][n] float32, the best first
+    parent: torch.Tensor                 # [groups][n] int32: beam of the group that it continues
+    token: torch.Tensor                  # [groups][n] int32
 
 
 def _on_device(t, name, device=None):
@@ -113,6 +122,44 @@ def _cache(pages, page_table=None):
     return kv
 
 
+def _by_heads(t, name, rows):
+    """Refuses what is not [rows][heads][head_dim] with a row's heads one after the other; the rows' stride."""
+    heads, hd = t.shape[1:]
+    if rows and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != hd) or (rows > 1 and t.stride(0) < heads * hd)):
+        raise ValueError(f"a row of {name} must hold its heads one after the other")
+    return t.stride(0) if rows > 1 else heads * hd
+
+
+def _queries(kv, q, pages, scale, out):
+    """Checks of an attention call's q, out and scale: (rows, heads, out, strides of q and out, scale)."""
+    dev, hd = pages.device, kv.head_dim
+    _on_device(q, "q", dev)
+    if q.dim() != 3 or q.dtype != pages.dtype or q.shape[2] != hd or q.shape[1] < 1 or q.shape[1] % kv.n_kv_heads:
+        raise ValueError("q must be [rows][a multiple of the cache's heads][head_dim] of the cache's type")
+    rows, heads, _ = q.shape
+    out = torch.empty((rows, heads, hd), dtype=q.dtype, device=dev) if out is None else out
+    _on_device(out, "out", dev)
+    if out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must be like q")
+    q_stride, out_stride = _by_heads(q, "q", rows), _by_heads(out, "out", rows)
+    if scale is None:
+        scale = 0.0                      # the library's default
+    elif ctypes.c_float(scale).value == 0:
+        raise ValueError("scale must not be 0 in fp32 (None is 1 / sqrt(head_dim))")
+    return rows, heads, out, q_stride, out_stride, scale
+
+
+def _sequences(kv, row_offsets, lengths, rows, max_rows, max_length, dev):
+    """(row_offsets, lengths, max_rows, max_length) as the library takes them."""
+    offs = lens = None
+    if kv.n_seqs:
+        offs = _indices(row_offsets, "row_offsets", (kv.n_seqs + 1,), dev)
+        lens = _indices(lengths, "lengths", (kv.n_seqs,), dev)
+    cap = kv.table_stride * PAGE
+    return (offs, lens, rows if max_rows is None else min(max_rows, rows),
+            cap if max_length is None else min(max_length, cap))
+
+
 def window_attention(q, pages, page_table, row_offsets, lengths, sinks=0, window=0, layer=0, scale=None,
                      max_rows=None, max_length=None, out=None):
     """Attention of one layer: row i of a sequence of r rows is the token at p = length - r + i and sees token t
@@ -126,36 +173,12 @@ def window_attention(q, pages, page_table, row_offsets, lengths, sinks=0, window
     last sequence are left as they were."""
     kv = _cache(pages, page_table)
     dev = pages.device
-    _on_device(q, "q", dev)
-    hd = kv.head_dim
-    if q.dim() != 3 or q.dtype != pages.dtype or q.shape[2] != hd or q.shape[1] < 1 or q.shape[1] % kv.n_kv_heads:
-        raise ValueError("q must be [rows][a multiple of the cache's heads][head_dim] of the cache's type")
-    rows, heads, _ = q.shape
-    out = torch.empty((rows, heads, hd), dtype=q.dtype, device=dev) if out is None else out
-    _on_device(out, "out", dev)
-    if out.shape != q.shape or out.dtype != q.dtype:
-        raise ValueError("out must be like q")
-    for t, name in ((q, "q"), (out, "out")):
-        if rows and (t.stride(2) != 1 or t.stride(1) != hd or (rows > 1 and t.stride(0) < heads * hd)):
-            raise ValueError(f"a row of {name} must hold its heads one after the other")
-    if kv.n_seqs:
-        offs = _indices(row_offsets, "row_offsets", (kv.n_seqs + 1,), dev)
-        lens = _indices(lengths, "lengths", (kv.n_seqs,), dev)
-    else:
-        offs = lens = None
-    max_rows = rows if max_rows is None else min(max_rows, rows)
-    cap = kv.table_stride * PAGE
-    max_length = cap if max_length is None else min(max_length, cap)
-    if scale is None:
-        scale = 0.0                      # the library's default
-    elif ctypes.c_float(scale).value == 0:
-        raise ValueError("scale must not be 0 in fp32 (None is 1 / sqrt(head_dim))")
+    rows, heads, out, q_stride, out_stride, scale = _queries(kv, q, pages, scale, out)
+    offs, lens, max_rows, max_length = _sequences(kv, row_offsets, lengths, rows, max_rows, max_length, dev)
     need = abi.tss_window_attn_bytes(kv, heads, rows, max_rows, max_length, sinks, window)
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    width = heads * hd
-    _call(dev, abi.tss_window_attn, kv, layer, q.data_ptr(), q.stride(0) if rows > 1 else width, heads, offs, lens,
-          rows, max_rows, max_length, sinks, window, scale, out.data_ptr(), out.stride(0) if rows > 1 else width,
-          ws.data_ptr() if need else None, need)
+    _call(dev, abi.tss_window_attn, kv, layer, q.data_ptr(), q_stride, heads, offs, lens, rows, max_rows, max_length,
+          sinks, window, scale, out.data_ptr(), out_stride, ws.data_ptr() if need else None, need)
     return out
 
 
@@ -164,6 +187,155 @@ def copy_pages(pages, src, dst):
     several copies, a destination appears once and is no source."""
     kv = _cache(pages)
     _call(pages.device, abi.tss_copy_pages, kv, src, dst)
+
+
+@functools.lru_cache(maxsize=64)
+def _frequencies(base, head_dim):
+    """base^(-2j / head_dim) for the head's pairs, as the library takes them."""
+    half = head_dim // 2
+    return (ctypes.c_double * half)(*(float(base) ** (-2.0 * j / head_dim) for j in range(half)))
+
+
+def append_kv(q, k, v, pages, page_table, row_offsets, lengths, positions=None, rope=10000.0, layer=0, max_rows=None,
+              out=None):
+    """Appends rows to one layer of the cache, rotated to their positions, and returns their rotated queries: row i of
+    a sequence of r rows is the token of slot lengths - r + i (rows and lengths as window_attention has them).
+
+    q: [rows][any heads][head_dim] (None: keys and values alone, returns None), k, v: [rows][the cache's
+    heads][head_dim], all of one type, float32, float16 or bfloat16; rows may be apart, as parts of one projection's
+    output are.  positions: int32 [rows], for rows whose position is not their slot (a tree's nodes).  rope: the
+    rotation's base, or its head_dim / 2 frequencies (host numbers), or None for no rotation.  max_rows: upper bound of
+    a sequence's rows.  out: the rotated queries, of the cache's type; may be q, otherwise shares no element with an
+    input.  Rows behind the last sequence and before token 0 are left as they were."""
+    kv = _cache(pages, page_table)
+    dev, hd = pages.device, kv.head_dim
+    for t, name in ((k, "k"), (v, "v")) + (() if q is None else ((q, "q"),)):
+        _on_device(t, name, dev)
+        if t.dim() != 3 or t.shape[2] != hd or t.dtype not in _TYPES or t.dtype != k.dtype or t.shape[0] != k.shape[0]:
+            raise ValueError("q, k and v must be [rows][heads][head_dim] of one type and number of rows")
+        if name != "q" and t.shape[1] != kv.n_kv_heads:
+            raise ValueError("k and v must have the cache's heads")
+    rows, heads = k.shape[0], 0 if q is None else q.shape[1]
+    q_at = q_out = None
+    q_stride = out_stride = 0
+    if heads:
+        out = torch.empty(q.shape, dtype=pages.dtype, device=dev) if out is None else out
+        _on_device(out, "out", dev)
+        if out.shape != q.shape or out.dtype != pages.dtype:
+            raise ValueError("out must be like q, of the cache's type")
+        q_at, q_out = q.data_ptr(), out.data_ptr()
+        q_stride, out_stride = _by_heads(q, "q", rows), _by_heads(out, "out", rows)
+    elif q is not None:
+        out = torch.empty(q.shape, dtype=pages.dtype, device=dev) if out is None else out
+    else:
+        out = None
+    offs, lens, max_rows, _ = _sequences(kv, row_offsets, lengths, rows, max_rows, None, dev)
+    pos = None if positions is None else _indices(positions, "positions", (rows,), dev)
+    if rope is None:
+        freq = None
+    elif not hasattr(rope, "__len__"):
+        rope = float(rope)
+        if not 0 < rope < float("inf"):
+            raise ValueError("the rotation's base must be positive and finite")
+        freq = _frequencies(rope, hd)
+    else:
+        freq = [float(x) for x in rope]
+        if len(freq) != hd // 2:
+            raise ValueError("rope must have head_dim / 2 frequencies")
+        freq = (ctypes.c_double * len(freq))(*freq)
+    _call(dev, abi.tss_append_kv, kv, layer, q_at, q_stride, heads, k.data_ptr(), _by_heads(k, "k", rows), v.data_ptr(),
+          _by_heads(v, "v", rows), _TYPES[k.dtype], offs, lens, pos, rows, max_rows, freq, q_out, out_stride)
+    return out
+
+
+def prefix_attention(q, pages, page_table, row_offsets, lengths, shared, group_offsets=None, layer=0, scale=None,
+                     max_rows=None, max_length=None, max_shared=None, max_group_rows=None, out=None):
+    """Attention of one layer for sequences that share a prefix: what window_attention gives without a window, but the
+    pages that a group of sequences has in common are read once for all of its rows.
+
+    shared: int32 [groups], how many first entries of the page tables of a group's sequences name the same pages.
+    group_offsets: int32 [groups + 1], a group's first sequences; None for one group of all (then shared has one entry).
+    max_shared and max_group_rows: upper bounds of a group's shared pages and rows (without them the page table's and
+    all of q's; tighter bounds launch less).  The other arguments are window_attention's."""
+    kv = _cache(pages, page_table)
+    dev = pages.device
+    rows, heads, out, q_stride, out_stride, scale = _queries(kv, q, pages, scale, out)
+    offs, lens, max_rows, max_length = _sequences(kv, row_offsets, lengths, rows, max_rows, max_length, dev)
+    if not isinstance(shared, torch.Tensor) or shared.dim() != 1:
+        raise ValueError("shared must be an int32 tensor [groups]")
+    groups = shared.shape[0]
+    shared = _indices(shared, "shared", shared.shape, dev)
+    if group_offsets is not None:
+        group_offsets = _indices(group_offsets, "group_offsets", (groups + 1,), dev)
+    elif groups != 1:
+        raise ValueError("several groups need group_offsets")
+    max_shared = kv.table_stride if max_shared is None else min(max_shared, kv.table_stride)
+    max_group_rows = rows if max_group_rows is None else min(max_group_rows, rows)
+    need = abi.tss_prefix_attn_bytes(kv, heads, rows, max_rows, max_length, groups, max_group_rows, max_shared)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _call(dev, abi.tss_prefix_attn, kv, layer, q.data_ptr(), q_stride, heads, offs, lens, rows, max_rows, max_length,
+          group_offsets, shared, groups, max_group_rows, max_shared, scale, out.data_ptr(), out_stride,
+          ws.data_ptr() if need else None, need)
+    return out
+
+
+def beam_select(logits, scores, n, ended=None, end_token=None):
+    """The n best continuations of each group of beams, by scores[beam] + log probability of the token.
+
+    logits: [groups * beams][vocab] float32, float16 or bfloat16, rows contiguous.  scores: float32 [groups][beams], at
+    most 32 beams.  ended: int32 [groups][beams], not 0 for a beam that has ended: its one candidate is end_token, with its
+    score as it is.  Returns BeamSelection, each [groups][n], n <= min(64, beams * vocab); ties go to the lower beam,
+    then to the lower token; see tss_beam_select for what is worth -inf."""
+    _on_device(logits, "logits")
+    dev = logits.device
+    if logits.dim() != 2 or logits.dtype not in _TYPES:
+        raise ValueError("logits must be [groups * beams][vocab] of float32, float16 or bfloat16")
+    rows, vocab = logits.shape
+    if vocab < 1 or (rows and vocab > 1 and logits.stride(1) != 1) or (rows > 1 and logits.stride(0) < vocab):
+        raise ValueError("rows of logits must be contiguous and must not overlap")
+    if not isinstance(scores, torch.Tensor) or scores.dim() != 2 or scores.dtype != torch.float32 \
+            or scores.device != dev or not scores.is_contiguous() or scores.numel() != rows:
+        raise ValueError("scores must be a contiguous float32 tensor [groups][beams], a score for each row of logits")
+    groups, beams = scores.shape
+    at = None
+    if ended is not None:
+        if end_token is None or not 0 <= end_token < vocab:
+            raise ValueError("beams that have ended need an end_token of the vocabulary")
+        at = _indices(ended, "ended", scores.shape, dev)
+    if not 1 <= beams <= abi.TSS_BEAMS_MAX or not 1 <= n <= min(abi.TSS_BEAMS_MAX_N, beams * vocab):
+        raise ValueError("at most 32 beams, and from 1 to min(64, beams * vocab) continuations")
+    i32 = torch.int32
+    score = torch.empty((groups, n), dtype=torch.float32, device=dev)
+    parent, token = torch.empty((groups, n), dtype=i32, device=dev), torch.empty((groups, n), dtype=i32, device=dev)
+    need = abi.tss_beam_select_bytes(groups, beams, vocab, n)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _call(dev, abi.tss_beam_select, logits.data_ptr(), _TYPES[logits.dtype], logits.stride(0) if rows > 1 else vocab,
+          groups, beams, vocab, scores.data_ptr(), at, end_token if at else 0, n, score.data_ptr(), parent.data_ptr(),
+          token.data_ptr(), ws.data_ptr() if need else None, need)
+    return BeamSelection(score, parent, token)
+
+
+def reorder_pages(pages, page_table, parents, lengths, shared=None, max_own=None):
+    """Sequence g * beams + b becomes what sequence g * beams + parents[g][b] was, in every layer and in place, all of a
+    group at once.
+
+    parents: int32 [groups][beams], at most 32 beams; page_table has groups * beams sequences.  lengths: int32 [groups *
+    beams], tokens of each sequence before the call.  shared: int32 [groups], first pages that the group's sequences have
+    in common, which stay (None: no page); the pages behind them must be each sequence's own.  max_own: upper bound
+    of the tokens behind the shared pages (None: the page table's; a tighter bound launches less).  The caller moves
+    its own lengths, lengths[parents]."""
+    kv = _cache(pages, page_table)
+    dev = pages.device
+    if not isinstance(parents, torch.Tensor) or parents.dim() != 2 or parents.numel() != kv.n_seqs:
+        raise ValueError("parents must be [groups][beams], an entry for each sequence of the page table")
+    groups, beams = parents.shape
+    if not 1 <= beams <= abi.TSS_BEAMS_MAX:
+        raise ValueError("from 1 to 32 beams")
+    par = _indices(parents, "parents", parents.shape, dev)
+    lens = _indices(lengths, "lengths", (kv.n_seqs,), dev)
+    at = None if shared is None else _indices(shared, "shared", (groups,), dev)
+    cap = kv.table_stride * PAGE
+    _call(dev, abi.tss_reorder_pages, kv, par, beams, lens, at, cap if max_own is None else min(max_own, cap))
 
 
 def pack_pages(k, v):

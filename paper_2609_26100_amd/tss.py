@@ -32,12 +32,14 @@ EXPORTS = (
     "tss_tree_meta", "tss_set_launch_mode", "tss_profile_kernel", "tss_profile_read", "tss_last_error", "tss_status_string",
     "tss_destroy", "tss_get_logits_device", "tss_get_attn_split", "tss_check_kv", "tss_verify_static",
     "tss_static_workspace_bytes", "tss_bf16_to_f16", "tss_token_logprobs", "tss_token_logprobs_bytes",
-    "tss_window_attn", "tss_window_attn_bytes", "tss_copy_pages", "tss_set_window", "tss_seq_fork", "tss_get_logprobs",
+    "tss_window_attn", "tss_window_attn_bytes", "tss_copy_pages", "tss_append_kv",
+    "tss_prefix_attn", "tss_prefix_attn_bytes", "tss_beam_select", "tss_beam_select_bytes", "tss_reorder_pages", "tss_set_window", "tss_seq_fork", "tss_get_logprobs",
 )
 
 TSS_STATIC_SCRATCH_BYTES = 64 << 20
 TSS_T_F32, TSS_T_BF16, TSS_T_F16 = 0, 1, 2
 TSS_LOGPROBS_MAX_TOKENS, TSS_LOGPROBS_MAX_TOP = 8, 32
+TSS_BEAMS_MAX, TSS_BEAMS_MAX_N = 32, 64
 
 
 class tss_model_cfg(ctypes.Structure):
@@ -104,6 +106,15 @@ def lib():
             "tss_window_attn_bytes": (SZ, [KV, I32, I32, I32, I32, I32, I32]),
             "tss_window_attn": (ctypes.c_int, [P, KV, I32, P, ctypes.c_int64, I32, P, P, I32, I32, I32, I32, I32,
                                                ctypes.c_float, P, ctypes.c_int64, P, SZ]),
+            "tss_append_kv": (ctypes.c_int, [P, KV, I32, P, ctypes.c_int64, I32, P, ctypes.c_int64, P, ctypes.c_int64,
+                                             I32, P, P, P, I32, I32, P, P, ctypes.c_int64]),
+            "tss_prefix_attn_bytes": (SZ, [KV, I32, I32, I32, I32, I32, I32, I32]),
+            "tss_prefix_attn": (ctypes.c_int, [P, KV, I32, P, ctypes.c_int64, I32, P, P, I32, I32, I32, P, P, I32, I32,
+                                               I32, ctypes.c_float, P, ctypes.c_int64, P, SZ]),
+            "tss_beam_select_bytes": (SZ, [I32, I32, I32, I32]),
+            "tss_beam_select": (ctypes.c_int, [P, P, I32, ctypes.c_int64, I32, I32, I32, P, P, I32, I32, P, P, P, P,
+                                               SZ]),
+            "tss_reorder_pages": (ctypes.c_int, [P, KV, P, I32, P, P, I32]),
             "tss_set_window": (ctypes.c_int, [P, I32, I32, I32]),
             "tss_seq_fork": (ctypes.c_int, [P, I32, P, I32, I32]),
             "tss_get_logprobs": (ctypes.c_int, [P, I32, P, I32, I32, P, P, P, P, P]),
@@ -138,7 +149,7 @@ def _ptr(a):
     return a.ctypes.data
 
 
-_PACK = [struct.Struct(f"{n}i").pack for n in range(8)]
+_PACK = [struct.Struct(f"{n}i").pack for n in range(9)]
 
 
 def _fit32(*numbers):
@@ -459,6 +470,48 @@ def tss_copy_pages(hip_stream, kv, src, dst):
     if s.ndim != 1 or s.shape != d.shape:
         raise ValueError("src and dst must be lists of one length")
     _check_op(lib().tss_copy_pages(hip_stream, kv, _ptr(s), _ptr(d), len(s)))
+
+
+def tss_append_kv(hip_stream, kv, layer, q, q_stride, n_q_heads, k, k_stride, v, v_stride, type, row_offsets, lengths,
+                  positions, rows, max_rows, inv_freq, q_out, q_out_stride):
+    """kv: a tss_paged_kv; inv_freq: None or a ctypes array of head_dim / 2 doubles; tensors are device addresses."""
+    _fit32(layer, n_q_heads, type, rows, max_rows)
+    _check_op(lib().tss_append_kv(hip_stream, kv, layer, q, q_stride, n_q_heads, k, k_stride, v, v_stride, type,
+                                  row_offsets, lengths, positions, rows, max_rows, inv_freq, q_out, q_out_stride))
+
+
+def tss_prefix_attn_bytes(kv, n_q_heads, rows, max_rows, max_length, n_groups, max_group_rows, max_shared) -> int:
+    _fit32(n_q_heads, rows, max_rows, max_length, n_groups, max_group_rows, max_shared)
+    return lib().tss_prefix_attn_bytes(kv, n_q_heads, rows, max_rows, max_length, n_groups, max_group_rows, max_shared)
+
+
+def tss_prefix_attn(hip_stream, kv, layer, q, q_stride, n_q_heads, row_offsets, lengths, rows, max_rows, max_length,
+                    group_offsets, shared, n_groups, max_group_rows, max_shared, scale, out, out_stride, workspace,
+                    workspace_bytes):
+    """kv: a tss_paged_kv; every tensor is a device address (or None)."""
+    _fit32(layer, n_q_heads, rows, max_rows, max_length, n_groups, max_group_rows, max_shared)
+    _check_op(lib().tss_prefix_attn(hip_stream, kv, layer, q, q_stride, n_q_heads, row_offsets, lengths, rows,
+                                    max_rows, max_length, group_offsets, shared, n_groups, max_group_rows, max_shared,
+                                    scale, out, out_stride, workspace, workspace_bytes))
+
+
+def tss_beam_select_bytes(n_groups, n_beams, vocab, n) -> int:
+    _fit32(n_groups, n_beams, vocab, n)
+    return lib().tss_beam_select_bytes(n_groups, n_beams, vocab, n)
+
+
+def tss_beam_select(hip_stream, logits, type, row_stride, n_groups, n_beams, vocab, scores, ended, end_token, n, score,
+                    parent, token, workspace, workspace_bytes):
+    """Every tensor is a device address (or None)."""
+    _fit32(type, n_groups, n_beams, vocab, end_token, n)
+    _check_op(lib().tss_beam_select(hip_stream, logits, type, row_stride, n_groups, n_beams, vocab, scores, ended,
+                                    end_token, n, score, parent, token, workspace, workspace_bytes))
+
+
+def tss_reorder_pages(hip_stream, kv, parents, n_beams, lengths, shared, max_own):
+    """kv: a tss_paged_kv; every tensor is a device address (or None)."""
+    _fit32(n_beams, max_own)
+    _check_op(lib().tss_reorder_pages(hip_stream, kv, parents, n_beams, lengths, shared, max_own))
 
 
 def tss_last_error(ctx) -> str:

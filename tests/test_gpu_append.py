@@ -1,0 +1,221 @@
+"""Rows appended to the paged cache against a plain 64-bit form: what is written, and that nothing else is."""
+import pytest
+import torch
+
+from paper_2609_26100_amd import ops
+from tests import beams_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+BITS = {torch.float16: torch.int16, torch.float32: torch.int32, torch.bfloat16: torch.int16}
+
+
+def bits(t):
+    return t.contiguous().view(BITS[t.dtype])
+
+
+class Case:
+    def __init__(self, lengths, rows, q_heads, heads, hd, kind, cache, seed=0, layers=1, behind=2, extra=0):
+        g = torch.Generator().manual_seed(seed + 31 * len(lengths) + hd)
+        self.lengths, self.rows, self.hd, self.kind, self.cache = lengths, rows, hd, kind, cache
+        per = max(1, max(-(-n // 16) for n in lengths))
+        total = len(lengths) * per + 3
+        self.table = torch.randperm(total, generator=g)[: len(lengths) * per].reshape(len(lengths), per).to(torch.int32)
+        self.pool = torch.randn(layers, total, 2, heads, 16 * hd, generator=g).to(ref.TYPES[cache])
+        n = sum(rows) + behind
+        self.qkv = torch.randn(n, q_heads + 2 * heads + extra, hd, generator=g).to(ref.TYPES[kind])
+        self.cut = [q_heads, heads, heads, extra]
+        self.layer = layers - 1
+
+    def parts(self, t):
+        return t.split(self.cut, 1)[:3]
+
+    def slots(self, max_rows=None):
+        """(row, sequence, slot) of every row that is taken."""
+        r0 = 0
+        for s, (n, length) in enumerate(zip(self.rows, self.lengths)):
+            for i in range(n):
+                p = length - n + i
+                if p >= 0 and (max_rows is None or i < max_rows):
+                    yield r0 + i, s, p
+            r0 += n
+
+    def run(self, positions=None, rope=10000.0, max_rows=None, no_q=False, in_place=False, out=None):
+        dev = self.pool.to(DEV)
+        q, k, v = self.parts(self.qkv.to(DEV))
+        off = torch.tensor([0] + list(torch.tensor(self.rows).cumsum(0)), dtype=torch.int32, device=DEV)
+        lens = torch.tensor(self.lengths, dtype=torch.int32, device=DEV)
+        pos = None if positions is None else torch.tensor(positions, dtype=torch.int32, device=DEV)
+        out = q if in_place else torch.full(q.shape, 7.0, dtype=dev.dtype, device=DEV) if out is None else out
+        got = ops.append_kv(None if no_q else q, k, v, dev, self.table.to(DEV), off, lens, positions=pos, rope=rope,
+                            layer=self.layer, max_rows=max_rows, out=None if no_q else out)
+        return dev, got
+
+    def check(self, positions=None, rope=10000.0, max_rows=None, no_q=False, in_place=False):
+        pool, out = self.run(positions, rope, max_rows, no_q, in_place)
+        pool = pool.cpu()
+        q, k, v = self.parts(self.qkv)
+        taken = list(self.slots(max_rows))
+        rows = torch.tensor([r for r, _, _ in taken], dtype=torch.long)
+        pos = torch.tensor([p for _, _, p in taken]) if positions is None else torch.tensor(positions)[rows]
+        freq = torch.zeros(self.hd // 2, dtype=torch.float64) if rope is None else \
+            ref.frequencies(self.hd, rope) if isinstance(rope, float) else torch.tensor(list(rope), dtype=torch.float64)
+        want = bits(self.pool).clone()
+        heads = k.shape[1]
+        kp = pool[self.layer, :, 0].view(-1, heads, 16, self.hd)
+        vw = want[self.layer, :, 1].view(-1, heads, 4, self.hd, 4)
+        kw = want[self.layer, :, 0].view(-1, heads, 16, self.hd)
+        turned, bound = ref.rotate(k[rows], pos, freq, self.cache)
+        for i, (r, s, p) in enumerate(taken):
+            page, t = int(self.table[s, p // 16]), p % 16
+            if not 0 <= page < self.pool.shape[1]:
+                continue
+            err = (kp[page, :, t].double() - turned[i]).abs()
+            assert (err <= bound[i]).all(), f"key of row {r}: {float((err / bound[i]).max())} of the bound"
+            kw[page, :, t] = bits(kp[page, :, t])
+            vw[page, :, t // 4, :, t % 4] = bits(v[r].to(pool.dtype))
+        assert torch.equal(bits(pool), want), "values, or something that was not to be written"
+        if no_q:
+            assert out is None
+            return
+        out = out.cpu()
+        turned, bound = ref.rotate(q[rows], pos, freq, self.cache)
+        err = (out[rows].double() - turned).abs()
+        assert (err <= bound).all(), f"queries: {float((err / bound).max())} of the bound"
+        rest = torch.ones(out.shape[0], dtype=torch.bool)
+        rest[rows] = False
+        left = q if in_place else torch.full_like(out, 7.0)
+        assert torch.equal(bits(out[rest]), bits(left[rest])), "rows that were not to be written"
+
+
+CASES = [
+    # lengths, rows, query heads, heads, hd
+    ([1], [1], 1, 1, 64),
+    ([17], [1], 32, 32, 128),
+    ([16, 17, 15, 33], [1, 1, 1, 1], 4, 2, 128),
+    ([40], [40], 6, 3, 64),
+    ([70, 3, 64, 0, 130], [5, 3, 16, 0, 37], 8, 2, 128),
+    ([5, 2], [9, 4], 3, 1, 64),                      # more rows than tokens
+    ([301, 299, 18], [100, 33, 17], 5, 5, 128),
+]
+
+
+@pytest.mark.parametrize("cache", ["f16", "f32"])
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("case", CASES)
+def test_against_64_bits(case, kind, cache):
+    Case(*case, kind, cache).check()
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_positions_far_and_negative(kind):
+    c = Case([33, 20], [9, 7], 4, 2, 128, kind, "f32", seed=1)
+    c.check(positions=[0, -1, 1, 17, -1000003, 999999, 1 << 24, 2 ** 31 - 1, -2 ** 31, 5, 5, 5, 4, 3, 2, 1, 0, 0])
+
+
+@pytest.mark.parametrize("rope", [None, 500000.0, "custom", 1.0])
+def test_rotations(rope):
+    for hd in (64, 128):
+        r = [0.5 ** j * (-1) ** j for j in range(hd // 2)] if rope == "custom" else rope
+        Case([100, 7], [50, 7], 3, 2, hd, "f32", "f16", seed=2).check(rope=r)
+
+
+def test_without_queries_and_bounds():
+    Case([50, 20], [20, 20], 4, 2, 64, "f16", "f16", seed=3).check(no_q=True)
+    Case([50, 20], [20, 20], 0, 2, 64, "f16", "f16", seed=3).check()
+    for n in (1, 3, 17, 100):
+        Case([50, 20], [20, 19], 4, 2, 128, "bf16", "f16", seed=4).check(max_rows=n)
+
+
+def test_strided_rows_and_in_place():
+    Case([50, 20], [20, 19], 4, 2, 128, "f16", "f16", seed=5, extra=3).check(in_place=True)
+    Case([50, 20], [20, 19], 4, 2, 64, "f32", "f32", seed=5, extra=1).check(in_place=True)
+    Case([50, 20], [20, 19], 4, 2, 64, "bf16", "f16", seed=5, extra=5).check()
+
+
+def test_layers_and_pages_outside_the_pool():
+    c = Case([100, 90], [60, 70], 2, 2, 128, "f32", "f16", seed=6, layers=3)
+    c.layer = 1
+    c.check()
+    c.table[0, 3], c.table[1, 2], c.table[1, 5] = -1, c.pool.shape[1], 2 ** 31 - 1
+    c.check()
+
+
+def test_behind_the_page_table():
+    """Slots that the page table does not reach are not written; their queries are."""
+    c = Case([40, 30], [30, 20], 2, 1, 64, "f32", "f16", seed=7)
+    c.table = c.table[:, :2].contiguous()
+    pool, out = c.run()
+    full = Case([40, 30], [30, 20], 2, 1, 64, "f32", "f16", seed=7)
+    whole, want = full.run()
+    assert torch.equal(bits(out.cpu()), bits(want.cpu()))
+    ids = c.table.flatten().long()
+    assert torch.equal(bits(pool.cpu()[:, ids]), bits(whole.cpu()[:, ids]))
+    rest = torch.ones(c.pool.shape[1], dtype=torch.bool)
+    rest[ids] = False
+    assert torch.equal(bits(pool.cpu()[:, rest]), bits(c.pool[:, rest]))
+
+
+def test_values_beyond_fp16_and_special():
+    c = Case([20], [20], 1, 1, 64, "f32", "f16", seed=8)
+    c.qkv[3, 2] = torch.tensor([1e30, -1e30, 65519.0, 65520.0, float("inf"), float("nan"), 1e-8, 6e-8] * 8)
+    pool, _ = c.run()
+    got = pool.cpu()[0, int(c.table[0, 0]), 1].view(1, 4, 64, 4)[0, 0, :, 3]
+    want = c.qkv[3, 2].half()
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got[~got.isnan()], want[~want.isnan()])
+
+
+def test_captured_and_replayed():
+    c = Case([50, 33], [5, 3], 4, 2, 128, "bf16", "f16", seed=9, behind=0)
+    pool, qkv = c.pool.to(DEV), c.qkv.to(DEV)
+    q, k, v = c.parts(qkv)
+    off = torch.tensor([0, 5, 8], dtype=torch.int32, device=DEV)
+    lens = torch.tensor(c.lengths, dtype=torch.int32, device=DEV)
+    table = c.table.to(DEV)
+    out = ops.append_kv(q, k, v, pool, table, off, lens, max_rows=8)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = ops.append_kv(q, k, v, pool, table, off, lens, max_rows=8)
+    for seed, lengths in ((1, [16, 8]), (2, [64, 3]), (3, [21, 48])):
+        fresh = Case(lengths, [5, 3], 4, 2, 128, "bf16", "f16", seed=seed, behind=0)
+        fresh.table, fresh.pool = c.table, c.pool
+        qkv.copy_(fresh.qkv.to(DEV))
+        pool.copy_(c.pool)
+        lens.copy_(torch.tensor(lengths, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        want_pool, want = fresh.run()
+        assert torch.equal(bits(pool), bits(want_pool)) and torch.equal(bits(out), bits(want))
+
+
+def test_on_a_stream_of_its_own():
+    c = Case([50, 33], [5, 3], 4, 2, 64, "f32", "f32", seed=10)
+    want_pool, want = c.run()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        pool, out = c.run()
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(bits(pool), bits(want_pool)) and torch.equal(bits(out), bits(want))
+
+
+def test_refusals():
+    c = Case([20], [4], 4, 2, 64, "f32", "f16")
+    q, k, v = (x.contiguous().to(DEV)[:4] for x in c.parts(c.qkv))
+    pool, table = c.pool.to(DEV), c.table.to(DEV)
+    off, lens = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in ([0, 4], [20]))
+    ok = dict(q=q, k=k, v=v, pages=pool, page_table=table, row_offsets=off, lengths=lens)
+    ops.append_kv(**ok)
+    for bad in (dict(q=q.half()), dict(v=v[:3]), dict(k=k[:, :1]), dict(q=q[..., :32]), dict(k=k.double()),
+                dict(q=q.transpose(0, 1)), dict(out=q), dict(lengths=lens.long()), dict(row_offsets=off[:1]),
+                dict(positions=off), dict(rope=0.0), dict(rope=float("nan")), dict(rope=[1.0] * 31),
+                dict(page_table=table[0]), dict(pages=pool.bfloat16())):
+        with pytest.raises(ValueError):
+            ops.append_kv(**dict(ok, **bad))
+    for bad in (dict(layer=1), dict(max_rows=-1), dict(rope=[float("inf")] * 32),
+                dict(q=torch.empty(4, 4 * 64 + 4, device=DEV)[:, :256].view(4, 4, 64)),
+                dict(k=torch.empty(4 * 128 + 2, device=DEV)[2:].view(4, 2, 64))):
+        with pytest.raises(ops.abi.TSSError):
+            ops.append_kv(**dict(ok, **bad))

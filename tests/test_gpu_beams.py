@@ -1,0 +1,187 @@
+"""The choice of the next beams against a plain 64-bit form: values, order, ties, beams that have ended or are lost."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_26100_amd import ops
+from tests import beams_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def make(groups, beams, vocab, kind, seed, spread=2.0):
+    g = torch.Generator().manual_seed(seed)
+    x = spread * torch.randn(groups * beams, vocab, generator=g)
+    x = (x + 1.5 * x.clamp_min(2.5)).to(ref.TYPES[kind])
+    return x, -3 * torch.rand(groups, beams, generator=g).cumsum(1) - 1
+
+
+def check(x, scores, n, ended=None, end=None, dev=None):
+    """x, scores, ended: CPU tensors; dev: x on the device, where its layout is another."""
+    dev = x.to(DEV) if dev is None else dev
+    r = ops.beam_select(dev, scores.to(DEV), n, ended=None if ended is None else ended.to(DEV), end_token=end)
+    groups, beams = scores.shape
+    for t, kind in ((r.score, torch.float32), (r.parent, torch.int32), (r.token, torch.int32)):
+        assert t.shape == (groups, n) and t.dtype == kind
+    score, parent, token = (t.cpu().numpy() for t in r)
+    xs = x.double().numpy().reshape(groups, beams, -1)
+    for g in range(groups):
+        v = ref.candidates(xs[g], scores[g].numpy(), None if ended is None else ended[g].numpy(), end)
+        ref.check_group(score[g], parent[g], token[g], v, n)
+    return r
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("groups,beams,vocab,n", [
+    (1, 1, 1, 1), (1, 1, 7, 5), (3, 2, 5, 10), (2, 4, 64, 8), (1, 4, 32000, 8), (2, 5, 8193, 10), (1, 32, 1001, 64),
+    (3, 3, 50021, 7), (1, 16, 20000, 32), (2, 2, 131072, 4), (65, 2, 333, 3), (1, 3, 262147, 64)])
+def test_against_64_bits(groups, beams, vocab, n, kind):
+    check(*make(groups, beams, vocab, kind, vocab + n), n)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_first_step(kind):
+    """Only a group's first beam is alive: its best tokens, all of parent 0."""
+    x, scores = make(3, 4, 5000, kind, 1)
+    scores[:, 0], scores[:, 1:] = 0.0, -torch.inf
+    r = check(x, scores, 8)
+    assert (r.parent == 0).all()
+
+
+def test_ended_beams():
+    x, scores = make(4, 5, 700, "f32", 2)
+    ended = torch.tensor([[1, 0, 0, 0, 1], [0, 0, 0, 0, 0], [1, 1, 1, 1, 1], [0, 1, 0, 9, -1]], dtype=torch.int32)
+    r = check(x, scores, 10, ended, 3)
+    # all ended: five candidates, then pairs of -inf by beam and token
+    assert r.parent[2].tolist() == [0, 1, 2, 3, 4, 0, 0, 0, 0, 0] and r.token[2].tolist() == [3] * 5 + [0, 1, 2, 4, 5]
+    assert torch.isneginf(r.score[2, 5:]).all()
+    x[:] = torch.nan                                 # an ended beam's logits do not matter
+    r = check(x, scores, 10, ended, 3)
+    assert r.score[0, :2].tolist() == [scores[0, 0].item(), scores[0, 4].item()]
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_ties(kind):
+    t = ref.TYPES[kind]
+    x = torch.zeros(6, 9000, dtype=t)                # everything equal
+    r = check(x, torch.zeros(2, 3), 40)
+    assert (r.parent == 0).all() and r.token[0].tolist() == list(range(40))
+    x, scores = make(1, 1, 3000, kind, 3)
+    x = x.repeat(4, 1)                               # four equal beams
+    r = check(x, torch.full((1, 4), -2.5), 16)
+    assert r.parent[0].tolist() == [0, 1, 2, 3] * 4
+    x = torch.full((4, 20000), -5.0, dtype=t)        # many equal ones at the cut
+    x[:, ::37] = 4.0
+    check(x, torch.tensor([[-1.0, -1.0, -1.5, -1.0]]), 64)
+    x[2, 19999], x[1, 77] = 4.0, 4.5
+    check(x, torch.tensor([[-1.0, -1.0, -1.5, -1.0]]), 64)
+
+
+def test_negative_zero_is_zero():
+    x = torch.full((1, 500), -1.0)
+    x[0, 400], x[0, 401], x[0, 30] = 0.0, -0.0, -0.0
+    r = check(x, torch.zeros(1, 1), 4)
+    assert r.token[0].tolist() == [30, 400, 401, 0]
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("vocab", [50, 20000, 70001])
+def test_masked_and_lost(kind, vocab):
+    x, scores = make(2, 6, vocab, kind, 4)
+    x[0, torch.randperm(vocab, generator=torch.Generator().manual_seed(5))[5:]] = -torch.inf   # five tokens left
+    x[1] = -torch.inf
+    x[2, vocab - 1] = torch.nan
+    x[3, 0] = torch.inf
+    scores[0, 4] = -torch.inf
+    scores[0, 5] = torch.nan
+    x[6:, 3:] = torch.finfo(ref.TYPES[kind]).min     # masked with the lowest value
+    scores[1, 2] = torch.inf
+    r = check(x, scores, 12)
+    assert (r.parent[0, :5] == 0).all() and torch.isneginf(r.score[0, 5:]).all()
+
+
+def test_nothing_left():
+    x, scores = torch.full((3, 40), -torch.inf), torch.zeros(1, 3)
+    r = check(x, scores, 50)
+    assert r.parent[0].tolist() == [0] * 40 + [1] * 10 and r.token[0].tolist() == list(range(40)) + list(range(10))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_far_values(kind):
+    """Logits and scores far from zero: the logarithm and the differences hold."""
+    x, scores = make(2, 4, 3000, kind, 6)
+    x = (x.float() * 1e5 if kind == "f32" else x.float() + 1000).to(ref.TYPES[kind])
+    check(x, scores - 1e4, 8)
+    x = torch.zeros(2, 3000)
+    x[0, 7], x[1, 9] = 3e38, -3e38
+    check(x, torch.tensor([[-1.0, -2.0]]), 8)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("skew,pad", [(0, 1), (1, 0), (3, 5), (7, 2)])
+def test_rows_that_are_not_aligned(kind, skew, pad):
+    x, scores = make(2, 3, 9001, kind, 7)
+    buf = torch.full((6 * (9001 + pad) + skew,), torch.nan, dtype=x.dtype, device=DEV)
+    dev = buf[skew:].view(6, 9001 + pad)[:, :9001]
+    dev.copy_(x)
+    check(x, scores, 6, dev=dev)
+
+
+def test_beyond_four_gib():
+    rows, vocab = 40, 60_000_000 // 64                # rows 240 MB apart
+    buf = torch.full((rows, 60_000_000), -100.0, dtype=torch.float32, device=DEV)
+    g = torch.Generator().manual_seed(8)
+    x = 3 * torch.randn(rows, 3000, generator=g)
+    buf[:, vocab - 3000:vocab] = x.to(DEV)
+    r = ops.beam_select(buf[:, :vocab], torch.zeros(5, 8, device=DEV), 16)
+    for i in range(5):
+        v = np.full((8, vocab), -100.0)
+        v[:, vocab - 3000:] = x[8 * i:8 * i + 8].numpy()
+        ref.check_group(r.score[i].cpu().numpy(), r.parent[i].cpu().numpy(), r.token[i].cpu().numpy(),
+                        ref.candidates(v, np.zeros(8)), 16)
+
+
+def test_captured_and_replayed():
+    x, scores = make(3, 4, 40000, "f16", 9)
+    dx, ds, de = x.to(DEV), scores.to(DEV), torch.zeros(3, 4, dtype=torch.int32, device=DEV)
+    ops.beam_select(dx, ds, 8, ended=de, end_token=2)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = ops.beam_select(dx, ds, 8, ended=de, end_token=2)
+    for seed in (10, 11, 12):
+        x, scores = make(3, 4, 40000, "f16", seed)
+        ended = torch.randint(0, 2, (3, 4), generator=torch.Generator().manual_seed(seed), dtype=torch.int32)
+        dx.copy_(x), ds.copy_(scores), de.copy_(ended)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = check(x, scores, 8, ended, 2)
+        assert all(torch.equal(a, b) for a, b in zip(r, want))
+
+
+def test_on_a_stream_of_its_own_and_again():
+    x, scores = make(5, 4, 50000, "bf16", 13)
+    dx, ds = x.to(DEV), scores.to(DEV)
+    want = ops.beam_select(dx, ds, 8)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = ops.beam_select(dx, ds, 8)
+    torch.cuda.current_stream().wait_stream(s)
+    for r in (got, ops.beam_select(dx, ds, 8)):
+        assert all(torch.equal(a, b) for a, b in zip(r, want))
+
+
+def test_refusals():
+    x, s = torch.zeros(8, 100, device=DEV), torch.zeros(2, 4, device=DEV)
+    e = torch.zeros(2, 4, dtype=torch.int32, device=DEV)
+    ops.beam_select(x, s, 8, e, 5)
+    for bad in (dict(logits=x.double()), dict(logits=x[0]), dict(logits=x.t()), dict(logits=x[:7]),
+                dict(scores=s.double()), dict(scores=s[0]), dict(scores=s.t()), dict(n=0), dict(n=65),
+                dict(ended=e.long()), dict(ended=e[:1]), dict(end_token=100), dict(end_token=-1), dict(end_token=None),
+                dict(scores=s.cpu())):
+        with pytest.raises(ValueError):
+            ops.beam_select(**dict(dict(logits=x, scores=s, n=8, ended=e, end_token=5), **bad))
+    assert ops.beam_select(x[:0], s[:0], 8).score.shape == (0, 8)
