@@ -172,10 +172,11 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void k_prefix(PrefixArgs args, P
 }
 
 // Virtual rows, the body and its blocks.
-Cut cut_of(bool f16, int64_t v_rows, int64_t heads, int64_t items, int most) {
+Cut cut_of(bool f16, int64_t v_rows, int most) {
   Cut c;
-  const int64_t shorts = heads * items * ((v_rows + 63) / 64);
-  c.body = !f16 || v_rows <= kFewRows ? 0 : v_rows <= 64 || shorts <= 256 || most < 2 ? 1 : 2;
+  // blocks of 128 rows where they hold the rows nearly as well as those of 64 do
+  const bool wide = most == 2 && (v_rows + 127) / 128 * 2 == (v_rows + 63) / 64;
+  c.body = !f16 || v_rows <= kFewRows ? 0 : wide ? 2 : 1;
   c.rows = body_rows(c.body);
   c.blocks = (int)((v_rows + c.rows - 1) / c.rows);
   c.splits = 1;
@@ -185,14 +186,14 @@ Cut cut_of(bool f16, int64_t v_rows, int64_t heads, int64_t items, int most) {
 PrefixPlan plan(bool f16, int n_heads, int group, int n_seqs, int max_rows, int max_length, int n_groups,
                 int max_group_rows, int max_shared) {
   PrefixPlan p;
-  p.shared = cut_of(f16, (int64_t)max_group_rows * group, n_heads, n_groups, 2);
-  p.own = cut_of(f16, (int64_t)max_rows * group, n_heads, n_seqs, 1);
+  p.shared = cut_of(f16, (int64_t)max_group_rows * group, 2);
+  p.own = cut_of(f16, (int64_t)max_rows * group, 1);
   const int64_t all = (max_length + kPage - 1) / kPage;
   if (n_groups == 0 || max_group_rows == 0 || max_shared == 0) p.shared.blocks = 0;
   const int64_t shared = p.shared.blocks ? std::min<int64_t>(max_shared, all) : 0;
   const int64_t own = std::max<int64_t>(1, all - shared);
   // the pages that a workgroup takes at least, and two workgroups a CU
-  auto least = [](const Cut& c) { return c.body == 0 ? 2 * kFewLeast : 2 * kRowsLeast; };
+  auto least = [](const Cut& c) { return c.body == 0 ? 16 : 12; };
   const int64_t ws = (int64_t)n_heads * n_groups * p.shared.blocks, wo = (int64_t)n_heads * n_seqs * p.own.blocks;
   const double work = (double)ws * shared + (double)wo * own;
   const double each = std::max(work / 512, 1.0);  // pages of a workgroup, if all were alike
