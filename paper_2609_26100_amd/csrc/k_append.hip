@@ -9,6 +9,9 @@
 // thread has eight dimensions of each half of a head's row, of q or K, or, of V, eight
 // dimensions of a group of four tokens, which the cache holds side by side: 16-byte
 // loads and stores, except where only some of the four are new.
+//
+// Bound by HBM for many rows (3500 rows of 40 + 2 x 40 heads of 128, fp32 to fp16, 323 MB: 60 us,
+// 5.3 TB/s), by a launch and three dependent loads for few (one row of 32 + 2 x 32 heads 5.2 us).
 #include "../../include/tss.h"
 #include "tss_internal.h"
 
@@ -19,36 +22,31 @@ namespace tss {
 namespace {
 
 constexpr int kAppendThreads = 256;
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-template <int TYPE> struct In;  // eight elements
-template <> struct In<TSS_T_F32> {
-  using T = float;
+// Eight elements: as they are loaded, and in fp32.
+template <int TYPE> struct Eight;
+template <> struct Eight<TSS_T_F32> {
   static constexpr int size = 4;
-  __device__ static void load(const void* p, float* x) {
-    const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
-    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  u32x4 w[2];
+  __device__ void load(const void* p) {
+    w[0] = ((const u32x4*)p)[0];
+    w[1] = ((const u32x4*)p)[1];
   }
+  __device__ float at(int e) const { return __uint_as_float(w[e / 4][e % 4]); }
 };
-template <> struct In<TSS_T_F16> {
+template <> struct Eight<TSS_T_F16> {
+  typedef _Float16 h8 __attribute__((ext_vector_type(8)));
   static constexpr int size = 2;
-  __device__ static void load(const void* p, float* x) {
-    typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-    const h8 h = *(const h8*)p;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)h[e];
-  }
+  h8 h;
+  __device__ void load(const void* p) { h = *(const h8*)p; }
+  __device__ float at(int e) const { return (float)h[e]; }
 };
-template <> struct In<TSS_T_BF16> {
+template <> struct Eight<TSS_T_BF16> {
   static constexpr int size = 2;
-  __device__ static void load(const void* p, float* x) {
-    const uint4 v = *(const uint4*)p;
-    const unsigned w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[2 * e] = __uint_as_float(w[e] << 16);
-      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-    }
-  }
+  u32x4 w;
+  __device__ void load(const void* p) { w = *(const u32x4*)p; }
+  __device__ float at(int e) const { return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16); }
 };
 
 // Eight elements to consecutive places, one rounding each.
@@ -68,7 +66,8 @@ __device__ __forceinline__ void store8(_Float16* p, const float* x) {
 // q, then K, then V) of a workgroup.
 template <typename T, int HD, int TYPE>
 __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a, int units) {
-  constexpr int ES = In<TYPE>::size, HALF = HD / 2, C = HALF / 8, VC = HD / 8;
+  using E = Eight<TYPE>;
+  constexpr int ES = E::size, HALF = HD / 2, C = HALF / 8, VC = HD / 8;
   __shared__ float2 s_cs[kPage][HALF + 1];
   const int s = blockIdx.y, tid = threadIdx.x;
   const int r0 = min(max(a.row_offsets[s], 0), a.rows);
@@ -81,82 +80,101 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a, int uni
   if (lo64 >= hi64) return;
   const int t0 = (int)(lo64 - page * kPage), nt = (int)(hi64 - lo64);  // first token of the page, how many
   const int row0 = r0 + (int)(lo64 - p0);                              // row of token t0
+  const int n_rot = a.n_q_heads + a.n_heads, u0 = blockIdx.z * units, u1 = min(u0 + units, n_rot + a.n_heads);
+  const int rot0 = min(u0, n_rot), v0 = max(u0, n_rot);
+  const int g0 = t0 / 4, groups = (t0 + nt - 1) / 4 - g0 + 1;
+  const int rots = (min(u1, n_rot) - rot0) * nt * C, vs = (u1 - v0) * groups * VC;
+
+  // item i of q and K: (head, token, chunk of 8 pairs); of V: (head, group of four tokens, chunk of
+  // 8 dimensions).  A thread's first item is requested before anything that waits for positions and
+  // page ids.
+  struct Rot { E x, y; };
+  struct Val { E x[4]; };
+  auto load_rot = [&](int i, Rot& q) {
+    if (i >= rots) return;
+    const int c = i % C, t = i / C % nt, u = rot0 + i / (C * nt);
+    const uint8_t* from =
+        u < a.n_q_heads ? (const uint8_t*)a.q + ((size_t)(row0 + t) * a.q_stride + (size_t)u * HD + c * 8) * ES
+                        : (const uint8_t*)a.k + ((size_t)(row0 + t) * a.k_stride + (size_t)(u - a.n_q_heads) * HD + c * 8) * ES;
+    q.x.load(from);
+    q.y.load(from + HALF * ES);
+  };
+  auto load_val = [&](int i, Val& q) {
+    if (i >= vs) return;
+    const int c = i % VC, g = g0 + i / VC % groups, h = v0 - n_rot + i / (VC * groups);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int t = min(max(g * 4 + e, t0), t0 + nt - 1);
+      q.x[e].load((const uint8_t*)a.v + ((size_t)(row0 + t - t0) * a.v_stride + (size_t)h * HD + c * 8) * ES);
+    }
+  };
+  Rot rot;
+  Val val;
+  load_rot(tid, rot);
+  if (rots == 0) load_val(tid, val);
+
   int id = -1;
   if (page < a.table_stride) id = a.page_table[(size_t)s * a.table_stride + page];
+  if (a.rotate && rots > 0) {
+    for (int i = tid; i < nt * HALF; i += kAppendThreads) {
+      const int t = i / HALF, j = i % HALF;
+      const int pos = a.positions ? a.positions[row0 + t] : (int)(lo64 + t);
+      const double x = (double)pos * a.turns[j];
+      const float y = 2.f * (float)(x - rint(x));
+      s_cs[t][j] = make_float2(cospif(y), sinpif(y));
+    }
+  }
+  __syncthreads();
   const bool there = (unsigned)id < (unsigned)a.n_pages;
   T* const kpage = (T*)a.kv_pages + (size_t)(there ? id : 0) * 2 * a.n_heads * (kPage * HD);
   T* const vpage = kpage + (size_t)a.n_heads * (kPage * HD);
 
-  for (int i = tid; i < nt * HALF; i += kAppendThreads) {
-    const int t = i / HALF, j = i % HALF;
-    float2 cs = make_float2(1.f, 0.f);
-    if (a.rotate) {
-      const int pos = a.positions ? a.positions[row0 + t] : (int)(lo64 + t);
-      const double x = (double)pos * a.turns[j];
-      const float y = 2.f * (float)(x - rint(x));
-      cs = make_float2(cospif(y), sinpif(y));
-    }
-    s_cs[t][j] = cs;
-  }
-  __syncthreads();
-
-  const int all = a.n_q_heads + 2 * a.n_heads;
-  const int u0 = blockIdx.z * units, u1 = min(u0 + units, all);
-  // q and K: item (head, token, chunk of 8 pairs)
-  const int rot0 = min(u0, a.n_q_heads + a.n_heads), rot1 = min(u1, a.n_q_heads + a.n_heads);
-  for (int i = tid; i < (rot1 - rot0) * nt * C; i += kAppendThreads) {
+  for (int i = tid; i < rots; i += kAppendThreads) {
+    if (i != tid) load_rot(i, rot);
+    const Rot& q = rot;
     const int c = i % C, t = i / C % nt, u = rot0 + i / (C * nt);
     const bool is_q = u < a.n_q_heads;
-    const int h = is_q ? u : u - a.n_q_heads, row = row0 + t;
     if (!is_q && !there) continue;
-    const uint8_t* from = (const uint8_t*)(is_q ? a.q : a.k) +
-                          ((size_t)row * (is_q ? a.q_stride : a.k_stride) + (size_t)h * HD + c * 8) * ES;
-    float x[8], y[8], z[8];
-    In<TYPE>::load(from, x);
-    In<TYPE>::load(from + HALF * ES, y);
+    float x[8], y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] = q.x.at(e);
+      y[e] = q.y.at(e);
+    }
     if (a.rotate) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float2 cs = s_cs[t][c * 8 + e];
-        z[e] = x[e] * cs.x - y[e] * cs.y;
+        const float z = x[e] * cs.x - y[e] * cs.y;
         y[e] = y[e] * cs.x + x[e] * cs.y;
+        x[e] = z;
       }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = x[e];
     }
-    T* to = (is_q ? (T*)a.q_out + (size_t)row * a.q_out_stride + (size_t)h * HD
-                  : kpage + (size_t)h * (kPage * HD) + (t0 + t) * HD) + c * 8;
-    store8(to, z);
+    T* to = (is_q ? (T*)a.q_out + (size_t)(row0 + t) * a.q_out_stride + (size_t)u * HD
+                  : kpage + (size_t)(u - a.n_q_heads) * (kPage * HD) + (t0 + t) * HD) + c * 8;
+    store8(to, x);
     store8(to + HALF, y);
   }
-  // V: item (head, group of four tokens, chunk of 8 dimensions)
   if (!there) return;
-  const int v0 = max(u0, a.n_q_heads + a.n_heads), v1 = u1;
-  const int g0 = t0 / 4, groups = (t0 + nt - 1) / 4 - g0 + 1;
-  for (int i = tid; i < (v1 - v0) * groups * VC; i += kAppendThreads) {
-    const int c = i % VC, g = g0 + i / VC % groups, h = v0 + i / (VC * groups) - a.n_q_heads - a.n_heads;
-    float x[4][8];
-    const int first = max(g * 4, t0), last = min(g * 4 + 4, t0 + nt);  // its new tokens
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int t = min(max(g * 4 + e, first), last - 1);
-      In<TYPE>::load((const uint8_t*)a.v + ((size_t)(row0 + t - t0) * a.v_stride + (size_t)h * HD + c * 8) * ES, x[e]);
-    }
+  for (int i = tid; i < vs; i += kAppendThreads) {
+    if (i != tid || rots > 0) load_val(i, val);
+    const Val& q = val;
+    const int c = i % VC, g = g0 + i / VC % groups, h = v0 - n_rot + i / (VC * groups);
     T* to = vpage + (size_t)h * (kPage * HD) + (g * HD + c * 8) * 4;
-    if (last - first == 4) {
+    if (g * 4 >= t0 && g * 4 + 4 <= t0 + nt) {
 #pragma unroll
       for (int d = 0; d < 8; d += 2) {
-        const float w[8] = {x[0][d],     x[1][d],     x[2][d],     x[3][d],
-                            x[0][d + 1], x[1][d + 1], x[2][d + 1], x[3][d + 1]};
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = q.x[e % 4].at(d + e / 4);
         store8(to + d * 4, w);
       }
-    } else {
+    } else {  // some of the four are new
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (g * 4 + e >= first && g * 4 + e < last)
+        if (g * 4 + e >= t0 && g * 4 + e < t0 + nt)
 #pragma unroll
-          for (int d = 0; d < 8; ++d) to[d * 4 + e] = (T)x[e][d];
+          for (int d = 0; d < 8; ++d) to[d * 4 + e] = (T)q.x[e].at(d);
     }
   }
 }
@@ -164,8 +182,11 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a, int uni
 template <typename T, int HD, int TYPE>
 hipError_t launch_typed(const AppendArgs& a, hipStream_t s) {
   const int all = a.n_q_heads + 2 * a.n_heads, tokens = std::min(a.max_rows, kPage);
-  const int units = std::max(1, kAppendThreads * 4 / (HD / 16 * tokens));
-  const dim3 grid((a.max_rows + 14) / kPage + 1, a.n_seqs, (all + units - 1) / units);
+  const int blocks = (a.max_rows + 14) / kPage + 1;
+  // two items a thread: one row of 96 heads takes 5.2 us (four: 6.9), 500 rows of 48 8.2 (one: 8.7),
+  // 3500 rows of 120 60 (one: 64, four: 65)
+  const int units = std::max(1, kAppendThreads * 2 / (HD / 16 * tokens));
+  const dim3 grid(blocks, a.n_seqs, (all + units - 1) / units);
   TSS_LAUNCH((k_append<T, HD, TYPE>), grid, dim3(kAppendThreads), 0, s, a, units);
   return hipGetLastError();
 }
