@@ -117,7 +117,7 @@ template <typename T, int HD, int BODY, typename A, typename S>
 __device__ __forceinline__ void run_block(const A& a, const Place& w, const Block& b, S& lds, float* part_o,
                                           float* part_ml) {
   if constexpr (BODY == 0)
-    few_block<T, HD, kRowsPages>(a, w, b, lds.few, part_o, part_ml);
+    few_block<T, HD, kRowsPages>(a, w, b, FewShared{lds.few.o, lds.few.m, lds.few.l}, part_o, part_ml);
   else
     rows_block<HD, BODY>(a, w, b, lds.ring, part_o, part_ml);
 }
@@ -128,7 +128,9 @@ template <typename T, int HD, int BP, int BO>
 __global__ __launch_bounds__(kPrefixThreads, 2) void k_prefix(PrefixArgs args, PrefixPlan p, int n_shared, float* part_o,
                                                              float* part_ml) {
   __shared__ __align__(16) union {
-    FewShared<kRowsPages> few;
+    struct {
+      float o[kRowsPages][kFewRows][64 + 4], m[kRowsPages][kFewRows], l[kRowsPages][kFewRows];
+    } few;
     uint8_t ring[BP || BO ? kRowsRing<HD> : 16];
   } lds;
   const int heads = args.n_heads;
@@ -174,7 +176,9 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void k_prefix(PrefixArgs args, P
 // Virtual rows, the body and its blocks.
 Cut cut_of(bool f16, int64_t v_rows, int most) {
   Cut c;
-  // blocks of 128 rows where they hold the rows nearly as well as those of 64 do
+  // blocks of 128 rows, which read a page half as often, where they hold the rows as well: 64
+  // sequences of 4 heads a kv head behind 32000 tokens 65 us, in blocks of 64 80; 160 rows (of
+  // which blocks of 128 leave more empty) behind 8000 32 us in either
   const bool wide = most == 2 && (v_rows + 127) / 128 * 2 == (v_rows + 63) / 64;
   c.body = !f16 || v_rows <= kFewRows ? 0 : wide ? 2 : 1;
   c.rows = body_rows(c.body);
@@ -192,13 +196,17 @@ PrefixPlan plan(bool f16, int n_heads, int group, int n_seqs, int max_rows, int 
   if (n_groups == 0 || max_group_rows == 0 || max_shared == 0) p.shared.blocks = 0;
   const int64_t shared = p.shared.blocks ? std::min<int64_t>(max_shared, all) : 0;
   const int64_t own = std::max<int64_t>(1, all - shared);
-  // the pages that a workgroup takes at least, and two workgroups a CU
-  auto least = [](const Cut& c) { return c.body == 0 ? 16 : 12; };
   const int64_t ws = (int64_t)n_heads * n_groups * p.shared.blocks, wo = (int64_t)n_heads * n_seqs * p.own.blocks;
-  const double work = (double)ws * shared + (double)wo * own;
-  const double each = std::max(work / 512, 1.0);  // pages of a workgroup, if all were alike
+  // Every workgroup about as many pages (a block of 128 rows takes twice as long for one), and
+  // as many of them as run at once, two a CU, or a little more than one a CU where their waves
+  // stream pages (8 beams of 32 heads behind 4000 tokens: 8 splits 20.6 us, 13 24.0); but no
+  // fewer pages than pay for a state (four beams behind 1008 tokens: 4 splits 10.5 us, 2 12.6;
+  // 8 of grouped heads behind 4000: 16 to 24 splits 12.4 to 12.9, 32 14.5).
+  auto weight = [](const Cut& c) { return c.body == 2 ? 2.0 : 1.0; };
+  const double each = ((double)ws * weight(p.shared) * shared + (double)wo * own) / (p.shared.body == 0 ? 300 : 512);
   auto splits = [&](const Cut& c, int64_t pages) {
-    const int64_t n = (int64_t)((double)pages / std::max<double>(each, least(c)) + 0.999);
+    const int least = c.body == 0 ? 16 : 12;
+    const int64_t n = (int64_t)((double)pages / std::max<double>(each / weight(c), least) + 0.999);
     return (int)std::max<int64_t>(1, std::min<int64_t>(n, kMaxSplits / 2));
   };
   p.shared.splits = splits(p.shared, shared);

@@ -45,7 +45,9 @@ namespace {
 // grid (kv head + heads * block, sequence, split)
 template <typename T, int HD, typename A>
 __global__ __launch_bounds__(kFewWaves * 64, 2) void k_window_few(A a, int splits, float* part_o, float* part_ml) {
-  __shared__ FewShared<kFewWaves> sh;
+  __shared__ float s_o[kFewWaves][kFewRows][64 + 4];
+  __shared__ float s_m[kFewWaves][kFewRows], s_l[kFewWaves][kFewRows];
+  const FewShared sh{s_o, s_m, s_l};
   const int block = blockIdx.x / a.n_heads;
   const Place w{(int)blockIdx.y, (int)blockIdx.x % a.n_heads, block, (int)gridDim.x / a.n_heads, (int)blockIdx.z,
                 splits, 0, splits > 1};

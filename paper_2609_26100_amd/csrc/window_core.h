@@ -56,11 +56,14 @@ __device__ __forceinline__ float sum4(float x) {
   return __uint_as_float(h[0]) + __uint_as_float(h[1]);
 }
 
-// S scale - m with the product rounded by itself (the empty asm keeps it out of an fma).
+// S scale - m with the product rounded by itself (the second empty asm keeps it out of an
+// fma; the first one keeps the products in the rare branch that needs them).
 __device__ __forceinline__ void round_exponents(f32x4& S, float scale, float m) {
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
-    float x = S[v] * scale;
+    float x = S[v];
+    asm volatile("" : "+v"(x));
+    x *= scale;
     asm volatile("" : "+v"(x));
     S[v] = x - m;
   }
@@ -331,15 +334,16 @@ struct Place {
   bool parts;  // states go to the workspace
 };
 
-template <int WAVES>
+// LDS of few_block, arrays of its kernel.
 struct FewShared {
-  float o[WAVES][kFewRows][64 + 4];
-  float m[WAVES][kFewRows], l[WAVES][kFewRows];
+  float (*o)[kFewRows][64 + 4];  // of each wave
+  float (*m)[kFewRows];
+  float (*l)[kFewRows];
 };
 
 // A block of up to 16 virtual rows by WAVES waves.
 template <typename T, int HD, int WAVES, typename A>
-__device__ __forceinline__ void few_block(const A& a, const Place& w, const Block& b, FewShared<WAVES>& sh, float* part_o,
+__device__ __forceinline__ void few_block(const A& a, const Place& w, const Block& b, const FewShared& sh, float* part_o,
                                           float* part_ml) {
   constexpr int PP = sizeof(T) == 2 ? 2 : 1;  // pages of a step
   constexpr int N = Page<T, HD>::N, NO = HD / 16;
@@ -623,10 +627,7 @@ __device__ __forceinline__ void rows_block(const A& a, const Place& w, const Blo
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();  // every wave's page of step st has landed, and step st - 1 has been read
     asm volatile("" ::: "memory");
-    if (st + 1 < n_st) {
-      if (((st + 1) & 15) == 0) load_ids(st + 1);
-      issue(st + 1);
-    }
+    if (st + 1 < n_st && ((st + 1) & 15) == 0) load_ids(st + 1);
   };
   // Step st.  EDGE: some of its tokens are seen by no row of the block.
   auto step = [&](int st, auto edge) {
@@ -636,23 +637,40 @@ __device__ __forceinline__ void rows_block(const A& a, const Place& w, const Blo
     f16x8 P[TILES][2];
     f32x4 S[TILES][kRowsPages];
 #pragma unroll
-    for (int p = 0; p < kRowsPages; ++p) {
+    for (int p = 0; p < kRowsPages; ++p)
 #pragma unroll
       for (int t = 0; t < TILES; ++t) S[t][p] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // pages and tiles inside: that many products are under way at once, and none waits for the last
 #pragma unroll
-      for (int c = 0; c < NK; ++c) {
+    for (int c = 0; c < NK; ++c) {
+#pragma unroll
+      for (int p = 0; p < kRowsPages; ++p) {
         const f16x8 k = *(const f16x8*)(base + (p * 2 * NK + c) * 1024);
 #pragma unroll
         for (int t = 0; t < TILES; ++t) S[t][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[t][c], S[t][p], 0, 0, 0);
       }
     }
+    // The next step's loads go out behind these products: in front of them the wave waited for the
+    // loads' queue and, while they landed, for its reads of K (a step of 128 rows 4560 cycles,
+    // now 3740).
+    if (st + 1 < n_st) issue(st + 1);
     // V is requested before the softmax, whose instructions hide it; the empty asm
-    // keeps the compiler from moving the reads down to their use
-    uint4 V[kRowsPages][NK];
+    // keeps the compiler from moving the reads down to their use.  Two pages' tokens of a dimension beside each other, as the product takes them, in reads
+    // of 8 bytes: read 16 at a time they would have to be moved, 48 moves a step.  Volatile, for
+    // the compiler joins reads otherwise.
+    typedef __attribute__((address_space(3))) uint8_t Lds;
+    typedef __attribute__((address_space(3))) f16x4 LdsHalfs;
+    f16x8 V[kRowsPages / 2][NK][2];
 #pragma unroll
-    for (int p = 0; p < kRowsPages; ++p)
+    for (int h = 0; h < kRowsPages / 2; ++h)
 #pragma unroll
-      for (int i = 0; i < NK; ++i) V[p][i] = *(const uint4*)(base + (p * 2 * NK + NK + i) * 1024);
+      for (int i = 0; i < NK; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const Lds* at = (const Lds*)base + (h * 4 * NK + NK + i) * 1024 + e * 8;
+          const f16x4 x = *(const volatile LdsHalfs*)at, y = *(const volatile LdsHalfs*)(at + 2 * NK * 1024);
+          V[h][i][e] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
     asm volatile("" ::: "memory");
     const bool whole = i1 <= span.all_last && (i1 < full_sinks || i0 >= span.all_first);
     if (EDGE || !whole) {
@@ -705,32 +723,30 @@ __device__ __forceinline__ void rows_block(const A& a, const Place& w, const Blo
           P[t][p >> 1][(p & 1) * 4 + v] = (_Float16)e;
         }
     }
-    uint4 keep[kRowsPages];
+    uint4 keep[kRowsPages / 2];
     if constexpr (EDGE) {
 #pragma unroll
-      for (int p = 0; p < kRowsPages; ++p) {
-        const uint2 k = keep16(b, b.page(min(i0 + p, b.n_pages - 1)) * kPage + 4 * grp, (there >> p) & 1);
-        keep[p] = uint4{k.x, k.y, k.x, k.y};
+      for (int h = 0; h < kRowsPages / 2; ++h) {
+        uint2 k[2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+          k[p] = keep16(b, b.page(min(i0 + 2 * h + p, b.n_pages - 1)) * kPage + 4 * grp, (there >> (2 * h + p)) & 1);
+        keep[h] = uint4{k[0].x, k[0].y, k[1].x, k[1].y};
       }
     }
     // two pages per MFMA: k = 8 grp + 4 b + u is token 4 grp + u of page 2 h + b
 #pragma unroll
     for (int h = 0; h < kRowsPages / 2; ++h)
 #pragma unroll
-      for (int i = 0; i < NK; ++i) {
-        uint4 va = V[2 * h][i], vb = V[2 * h + 1][i];
-        if constexpr (EDGE) {
-          va = both(va, keep[2 * h]);
-          vb = both(vb, keep[2 * h + 1]);
-        }
-        const f16x8 v0 = __builtin_bit_cast(f16x8, uint4{va.x, va.y, vb.x, vb.y});
-        const f16x8 v1 = __builtin_bit_cast(f16x8, uint4{va.z, va.w, vb.z, vb.w});
+      for (int i = 0; i < NK; ++i)
 #pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-          O[t][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, P[t][h], O[t][2 * i], 0, 0, 0);
-          O[t][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, P[t][h], O[t][2 * i + 1], 0, 0, 0);
+        for (int e = 0; e < 2; ++e) {
+          f16x8 v = V[h][i][e];
+          if constexpr (EDGE) v = __builtin_bit_cast(f16x8, both(__builtin_bit_cast(uint4, v), keep[h]));
+#pragma unroll
+          for (int t = 0; t < TILES; ++t)
+            O[t][2 * i + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, P[t][h], O[t][2 * i + e], 0, 0, 0);
         }
-      }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // step st has been read (see arrive)
   };
   auto clean = [&](int st) {
@@ -743,6 +759,7 @@ __device__ __forceinline__ void rows_block(const A& a, const Place& w, const Blo
   if (n_st > 0) arrive(0);
   while (st < n_st) {
     if (!on) {
+      if (st + 1 < n_st) issue(st + 1);
       if (++st < n_st) arrive(st);
       continue;
     }
