@@ -252,8 +252,8 @@ int tss_verify(tss_ctx* ctx, int32_t seq, const int32_t* draft_tokens, const int
  * contents: calls that overlap on one GPU (from several host threads, or on
  * streams that run at the same time) race, and the caller must serialise
  * them.  The merge counters are cleared at the start of every step.
- * tss_get_logits, tss_get_logits_device, tss_get_greedy, tss_get_logprobs and
- * tss_get_attn_split read the last step's workspace (and write nothing there),
+ * tss_get_logits, tss_get_logits_device, tss_get_greedy, tss_get_logprobs,
+ * tss_get_beams and tss_get_attn_split read the last step's workspace (and write nothing there),
  * so after a static call they are valid only until the next call on that GPU
  * reuses the scratch. */
 #define TSS_STATIC_SCRATCH_BYTES ((size_t)64 << 20)
@@ -365,6 +365,24 @@ int tss_seq_truncate(tss_ctx* ctx, int32_t seq, int32_t n_kv);
  * TSS_EINVAL for unknown, repeated or equal sequences.  Paper: Problem
  * Formulation (several continuations of one cached prefix). */
 int tss_seq_fork(tss_ctx* ctx, int32_t src, const int32_t* dst, int32_t n_dst, int32_t n_kv);
+
+/* Sequences seqs[0 .. n) change places, all at once: seqs[i] becomes what
+ * seqs[parents[i]] was (any map: several may continue one, exchanges too), its
+ * tokens, skip mask and window.  The first `first` tokens, at most the shortest one's, must be
+ * the same in all of them (forks of one prompt) and stay where they are; the pages
+ * behind them are moved on the device, in place, on the context's stream (without
+ * waiting; later calls are ordered behind).  TSS_EINVAL for unknown or repeated
+ * sequences, more than 32, a parent outside [0, n), another `first`.  Paper: Problem
+ * Formulation (several continuations of one prefix). */
+int tss_seq_reorder(tss_ctx* ctx, const int32_t* seqs, const int32_t* parents, int32_t n, int32_t first);
+
+/* The n best continuations of each group of beams, from the logits of the last
+ * verify's rows 0 .. n_groups * n_beams - 1 (a step of one-node drafts, a beam each), to
+ * host memory; returns when they are there.  All arrays are on the host; limits,
+ * arguments, results and their order as tss_beam_select has them.  Scratch and
+ * errors as tss_get_logprobs.  Paper: as tss_beam_select. */
+int tss_get_beams(tss_ctx* ctx, int32_t n_groups, int32_t n_beams, const float* scores, const int32_t* ended,
+                  int32_t end_token, int32_t n, float* score, int32_t* parent, int32_t* token);
 
 /* Log probabilities of given tokens, entropy and the top_k alternatives of the
  * last verify's rows 0 .. n_nodes - 1 (rows in the step's node order), from its

@@ -67,14 +67,15 @@ __global__ __launch_bounds__(kCopyThreads, B <= 8 ? 8 : B <= 16 ? 6 : 3) void k_
                                                                                           int pieces) {
   const int g = blockIdx.y, l = blockIdx.z, lane = threadIdx.x & 63;
   if (!((a.layers[l >> 6] >> (l & 63)) & 1ull)) return;
-  const int first = a.shared ? min(max(a.shared[g], 0), a.table_stride) : 0;
+  const int first = a.shared ? min(max(a.shared[g], 0), a.table_stride) : a.first;
   const int pg = first + (int)(blockIdx.x / pieces);
   if (pg >= a.table_stride) return;
   // lane b: beam b of the group
-  const int seq = g * a.n_beams + min(lane, a.n_beams - 1);
-  int parent = a.parents[seq];
+  const int beam = min(lane, a.n_beams - 1), at_seq = g * a.n_beams + beam;
+  const int seq = a.parents ? at_seq : a.seq[beam];
+  int parent = a.parents ? a.parents[at_seq] : a.parent[beam];
   const int id = a.page_table[(size_t)seq * a.table_stride + pg];
-  const int len = a.lengths[seq];
+  const int len = a.parents ? a.lengths[at_seq] : a.length[beam];
   const bool there = (unsigned)id < (unsigned)a.n_pages;
   const uint64_t full = __ballot(lane < a.n_beams && there && pg * kPage < len);  // a page to take
   const bool moves = lane < a.n_beams && there && (unsigned)parent < (unsigned)a.n_beams && parent != lane &&
@@ -108,7 +109,7 @@ hipError_t launch_reorder(const ReorderArgs& a, hipStream_t s) {
   const int64_t pieces = pieces_of(a);
   // a page has whole pieces: a head's K alone is 2 KiB, and V as much
   if (a.page_bytes % kReorderPiece != 0 || a.table_stride > INT32_MAX / kPage || a.n_groups < 1 || a.n_beams < 1 ||
-      a.n_beams > 32 || a.n_layers < 1 || a.n_layers > kMaxLayers || a.max_own < 1 || !reorder_fits(a))
+      a.n_beams > kMaxBeams || (!a.parents && a.n_groups != 1) || a.first < 0 || a.n_layers < 1 || a.n_layers > kMaxLayers || a.max_own < 1 || !reorder_fits(a))
     return hipErrorInvalidValue;
   const dim3 grid(pieces * pages_of(a), a.n_groups, a.n_layers), block(kCopyThreads);
   if (a.n_beams <= 4)

@@ -1901,6 +1901,123 @@ int tss_seq_fork(tss_ctx* c, int32_t src, const int32_t* dst, int32_t n_dst, int
   return TSS_OK;
 }
 
+int tss_seq_reorder(tss_ctx* c, const int32_t* seqs, const int32_t* parents, int32_t n, int32_t first) {
+  if (!c) return TSS_EINVAL;
+  if (n < 1 || n > kMaxBeams || !seqs || !parents) return fail(c, TSS_EINVAL, "from 1 to 32 sequences to reorder");
+  for (int i = 0; i < n; ++i) {
+    const int r = check_ready(c, seqs[i]);
+    if (r) return r;
+    if (parents[i] < 0 || parents[i] >= n) return fail(c, TSS_EINVAL, "a parent is no entry of the list");
+    for (int j = 0; j < i; ++j)
+      if (seqs[j] == seqs[i]) return fail(c, TSS_EINVAL, "a sequence appears twice");
+  }
+  const tss_model_cfg& cf = c->cfg;
+  ReorderArgs a{};
+  a.pages = c->kv + c->kvl.pages;
+  a.page_bytes = (size_t)2 * cf.n_heads * kPage * cf.head_dim * c->es;
+  a.layer_bytes = a.page_bytes * c->kvl.n_pages;
+  a.n_layers = cf.n_layers;
+  a.page_table = (const int32_t*)(c->kv + c->kvl.page_table);
+  a.n_pages = c->kvl.n_pages;
+  a.n_groups = 1;
+  a.n_beams = n;
+  a.table_stride = c->kvl.pages_per_seq;
+  a.first = first / kPage;
+  bool any = false;
+  for (int i = 0; i < n; ++i) {
+    if (first < 0 || first > c->n_kv[seqs[i]])
+      return fail(c, TSS_EINVAL, "first exceeds a sequence's tokens");
+    a.seq[i] = seqs[i];
+    a.parent[i] = parents[i];
+    a.length[i] = c->n_kv[seqs[i]];
+    if (parents[i] == i) continue;
+    a.max_own = std::max(a.max_own, c->n_kv[seqs[parents[i]]] - a.first * kPage);
+    for (int l = 0; l < cf.n_layers; ++l)  // layers without K/V have nothing to move
+      if (c->kv_len[seqs[parents[i]]][l] > 0) {
+        a.layers[l >> 6] |= 1ull << (l & 63);
+        any = true;
+      }
+  }
+  try {
+    // the states first, so that nothing fails behind the launch
+    std::vector<int32_t> n_kv(n);
+    std::vector<decltype(c->kv_len)::value_type> kv_len(n);
+    std::vector<decltype(c->mask)::value_type> mask(n);
+    std::vector<decltype(c->window)::value_type> window(n);
+    for (int i = 0; i < n; ++i) {
+      const int s = seqs[parents[i]];
+      n_kv[i] = c->n_kv[s];
+      kv_len[i] = c->kv_len[s];
+      mask[i] = c->mask[s];
+      window[i] = c->window[s];
+    }
+    if (any && a.max_own > 0) {
+      if (!launch_reorder || !reorder_fits(a)) return fail(c, TSS_EINVAL, "built without the operators' kernels");
+      HIPCHK(launch_reorder(a, c->stream), "reordering");
+    }
+    for (int i = 0; i < n; ++i) {
+      c->n_kv[seqs[i]] = n_kv[i];
+      std::swap(c->kv_len[seqs[i]], kv_len[i]);
+      std::swap(c->mask[seqs[i]], mask[i]);
+      c->window[seqs[i]] = window[i];
+    }
+  } catch (...) {
+    return fail(c, TSS_ENOSPACE, "no host memory");
+  }
+  return TSS_OK;
+}
+
+int tss_get_beams(tss_ctx* c, int32_t n_groups, int32_t n_beams, const float* scores, const int32_t* ended,
+                  int32_t end_token, int32_t n, float* score, int32_t* parent, int32_t* token) {
+  if (!c) return TSS_EINVAL;
+  if (c->poisoned) return fail(c, TSS_ESTATE, "context poisoned by an earlier HIP error");
+  const int V = c->cfg.vocab;
+  if (n_groups < 1 || n_beams < 1 || n_beams > TSS_BEAMS_MAX || (int64_t)n_groups * n_beams > c->last_M)
+    return fail(c, TSS_EINVAL, "the beams exceed 32 a group or the last verify's nodes");
+  if (n < 1 || n > TSS_BEAMS_MAX_N || n > (int64_t)n_beams * V)
+    return fail(c, TSS_EINVAL, "n outside [1, min(64, n_beams * vocab)]");
+  if (!scores || !score || !parent || !token) return fail(c, TSS_EINVAL, "null array");
+  if (ended && (end_token < 0 || end_token >= V)) return fail(c, TSS_EINVAL, "end_token outside the vocabulary");
+  if (!launch_beams || !beams_fit(n_groups, n_beams, V)) return fail(c, TSS_EINVAL, "vocabulary too large");
+  // scratch as tss_get_logprobs has it: scores and ended beams, the results, the call's own
+  const size_t rows = (size_t)n_groups * n_beams, nc = (size_t)n_groups * n, words = 2 * rows + 3 * nc;
+  const size_t own = align256(words * 4), need = own + beams_bytes(n_groups, n_beams, V, n);
+  if (need > c->wsl_own.part_slots * 64 * c->cfg.head_dim * 4)
+    return fail(c, TSS_ENOSPACE, "the workspace has no room for that many beams");
+  uint8_t* base = c->ws_own + c->wsl_own.part_o;
+  float* dev = (float*)base;
+  BeamArgs a{};
+  a.x = c->out_ws + c->out_wsl.logits;
+  a.stride = V;
+  a.n_groups = n_groups;
+  a.n_beams = n_beams;
+  a.vocab = V;
+  a.type = TSS_T_F32;
+  a.scores = dev;
+  a.ended = ended ? (const int32_t*)(dev + rows) : nullptr;
+  a.end_token = end_token;
+  a.n = n;
+  a.score = dev + 2 * rows;
+  a.parent = (int32_t*)(a.score + nc);
+  a.token = a.parent + nc;
+  std::vector<int32_t> host;
+  try {
+    host.resize(words);
+  } catch (...) {
+    return fail(c, TSS_ENOSPACE, "no host memory");
+  }
+  std::memcpy(host.data(), scores, rows * 4);
+  if (ended) std::memcpy(host.data() + rows, ended, rows * 4);
+  HIPCHK(hipMemcpyAsync(dev, host.data(), 2 * rows * 4, hipMemcpyHostToDevice, c->stream), "beams");
+  HIPCHK(launch_beams(a, base + own, c->stream), "choice of beams");
+  HIPCHK(hipMemcpyAsync(host.data() + 2 * rows, a.score, 3 * nc * 4, hipMemcpyDeviceToHost, c->stream), "results");
+  HIPCHK(hipStreamSynchronize(c->stream), "choice of beams");
+  std::memcpy(score, host.data() + 2 * rows, nc * 4);
+  std::memcpy(parent, host.data() + 2 * rows + nc, nc * 4);
+  std::memcpy(token, host.data() + 2 * rows + 2 * nc, nc * 4);
+  return TSS_OK;
+}
+
 int tss_get_logprobs(tss_ctx* c, int32_t n_nodes, const int32_t* tokens, int32_t n_tokens, int32_t top_k,
                      float* logprob, int32_t* rank, float* entropy, float* top_logprob, int32_t* top_token) {
   if (!c) return TSS_EINVAL;

@@ -531,12 +531,17 @@ TSS_WEAK bool beams_fit(int n_groups, int n_beams, int vocab);
 TSS_WEAK size_t beams_bytes(int n_groups, int n_beams, int vocab, int n);
 TSS_WEAK hipError_t launch_beams(const BeamArgs& a, void* workspace, hipStream_t s);
 
+constexpr int kMaxBeams = 32;  // sequences that are reordered together
 struct ReorderArgs {
   uint8_t* pages;
   size_t page_bytes, layer_bytes;
   uint64_t layers[kMaxLayers / 64];  // bit l: layer l takes part
   const int32_t *page_table, *parents, *lengths, *shared;
   int n_layers, n_pages, n_groups, n_beams, table_stride, max_own;
+  // one group whose sequences, parents and lengths come by value (parents null), behind
+  // `first` pages
+  int first;
+  int32_t seq[kMaxBeams], parent[kMaxBeams], length[kMaxBeams];
 };
 TSS_WEAK bool reorder_fits(const ReorderArgs& a);
 TSS_WEAK hipError_t launch_reorder(const ReorderArgs& a, hipStream_t s);

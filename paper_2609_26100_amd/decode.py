@@ -13,6 +13,11 @@ autoregressive_decode: the plain greedy loop, one token per verify step (a
 one-node draft: the root alone), the baseline both for the output and for
 throughput.
 
+beam_decode: beam search under the request's skip mask and window.  The beams are
+forks of the sequence that go through the decoder together, one node each in a
+batched step; the best continuations are chosen from the step's logits on the device
+and the beams' cached tokens behind the prompt are reordered in place.
+
 A drafter is any callable drafter(root, pos) -> (tokens, parent) with
 tokens[0] == root, parent[0] == -1 (parent None = chain), where pos counts
 the tokens generated so far.  The loop's own host work per step is a
@@ -125,3 +130,53 @@ def autoregressive_decode(verifier, seq, root, max_new, mask=None, logprobs=None
         root = int(nt)
     return DecodeResult(np.asarray(out, dtype=np.int32), max_new, [0] * max_new, time.perf_counter() - t0,
                         logprobs=lps.result(max_new) if lps is not None else None)
+
+
+@dataclass
+class BeamResult:
+    tokens: list                   # of each beam, the best first: int32 arrays, up to and with end_token
+    scores: np.ndarray             # sums of the tokens' log probabilities
+    ended: np.ndarray              # whether the beam ends with end_token
+    steps: int
+
+
+def beam_decode(verifier, seq, root, max_new, beams, end_token=None):
+    """Beam search after `root` (the last prompt token, whose K/V are not cached yet): the len(beams) most probable
+    continuations found, of at most max_new tokens, or shorter ones that end with end_token.
+
+    beams: sequences of the verifier, other than seq, whose contents may be replaced, one for each beam, at most
+    max_batch.  They take seq's skip mask and window; seq itself stays as it is.  A score of -inf is no continuation
+    (fewer tokens with a finite logit than beams)."""
+    beams = [int(s) for s in abi._int32s(beams, "beams")]
+    n = len(beams)
+    if not 1 <= n <= min(verifier.cfg.max_batch, abi.TSS_BEAMS_MAX) or len(set(beams)) < n or seq in beams:
+        raise ValueError("beams must be from 1 to max_batch different sequences other than the decoded one")
+    vocab = verifier.cfg.vocab
+    if end_token is not None and not 0 <= end_token < vocab:
+        raise ValueError("end_token outside the vocabulary")
+    base = verifier.length(seq)
+    if base + max_new > verifier.max_tokens:
+        raise ValueError("the beams' sequences have no room for that many tokens")
+    verifier.fork(seq, beams)
+    scores = np.full((1, n), -np.inf, np.float32)
+    scores[0, 0] = 0
+    ended = np.zeros((1, n), np.int32)
+    history = np.empty((n, 0), np.int32)
+    roots = np.full(n, root, np.int32)
+    steps = 0
+    while steps < max_new and not ended.all():
+        verifier.verify_batch(beams, list(roots[:, None]), commit=steps + 1 < max_new)
+        scores, parent, roots = verifier.beams(scores, n, None if end_token is None else ended, end_token or 0)
+        parent, roots = parent[0], roots[0]
+        steps += 1
+        if steps < max_new:
+            verifier.reorder(beams, parent, base)
+        history = np.concatenate([history[parent], roots[:, None]], 1)
+        if end_token is not None:
+            ended = (ended[:, parent] != 0) | (roots == end_token)[None]
+            ended = ended.astype(np.int32)
+    tokens = []
+    for h in history:
+        at = np.flatnonzero(h == end_token) if end_token is not None else ()
+        tokens.append(h[: at[0] + 1].copy() if len(at) else h.copy())
+    return BeamResult(tokens, scores[0], ended[0] != 0, steps)

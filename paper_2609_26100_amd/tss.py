@@ -34,6 +34,7 @@ EXPORTS = (
     "tss_static_workspace_bytes", "tss_bf16_to_f16", "tss_token_logprobs", "tss_token_logprobs_bytes",
     "tss_window_attn", "tss_window_attn_bytes", "tss_copy_pages", "tss_append_kv",
     "tss_prefix_attn", "tss_prefix_attn_bytes", "tss_beam_select", "tss_beam_select_bytes", "tss_reorder_pages", "tss_set_window", "tss_seq_fork", "tss_get_logprobs",
+    "tss_seq_reorder", "tss_get_beams",
 )
 
 TSS_STATIC_SCRATCH_BYTES = 64 << 20
@@ -119,6 +120,8 @@ def lib():
             "tss_seq_fork": (ctypes.c_int, [P, I32, P, I32, I32]),
             "tss_get_logprobs": (ctypes.c_int, [P, I32, P, I32, I32, P, P, P, P, P]),
             "tss_copy_pages": (ctypes.c_int, [P, KV, P, P, I32]),
+            "tss_seq_reorder": (ctypes.c_int, [P, P, P, I32, I32]),
+            "tss_get_beams": (ctypes.c_int, [P, I32, I32, P, P, I32, I32, P, P, P]),
             "tss_get_path": (ctypes.c_int, [P, I32, P, ctypes.POINTER(I32)]),
             "tss_seq_length": (ctypes.c_int, [P, I32, ctypes.POINTER(I32)]),
             "tss_seq_truncate": (ctypes.c_int, [P, I32, I32]),
@@ -402,6 +405,31 @@ def tss_get_logprobs(ctx, n_nodes, tokens=None, top_k=0):
     _check(lib().tss_get_logprobs(ctx, n_nodes, _ptr(t), n, top_k, _ptr(lp), _ptr(rank), _ptr(ent), _ptr(top_lp),
                                   _ptr(top_tok)), ctx, "tss_get_logprobs")
     return lp, rank, ent, top_lp, top_tok
+
+
+def tss_seq_reorder(ctx, seqs, parents, first):
+    _fit32(first)
+    q, p = _int32s(seqs, "seqs"), _int32s(parents, "parents")
+    if q.ndim != 1 or q.shape != p.shape:
+        raise ValueError("seqs and parents must be lists of one length")
+    _check(lib().tss_seq_reorder(ctx, _ptr(q), _ptr(p), len(q), first), ctx, "tss_seq_reorder")
+
+
+def tss_get_beams(ctx, scores, n, ended=None, end_token=0):
+    """Returns (score, parent, token) [groups][n] of scores [groups][beams] and the last verify's first groups * beams
+    rows; ended: None or like scores, not 0 for a beam that has ended."""
+    _fit32(n, end_token)
+    s = np.ascontiguousarray(scores, dtype=np.float32)
+    if s.ndim != 2:
+        raise ValueError("scores must be [groups][beams]")
+    e = None if ended is None else _int32s(ended, "ended")
+    if e is not None and e.shape != s.shape:
+        raise ValueError("ended must be like scores")
+    shape = (s.shape[0], max(n, 0))
+    score, parent, token = np.empty(shape, np.float32), np.empty(shape, np.int32), np.empty(shape, np.int32)
+    _check(lib().tss_get_beams(ctx, s.shape[0], s.shape[1], _ptr(s), _ptr(e), end_token, n, _ptr(score), _ptr(parent),
+                               _ptr(token)), ctx, "tss_get_beams")
+    return score, parent, token
 
 
 def tss_validate_tree(parent, n_nodes, max_nodes) -> int:

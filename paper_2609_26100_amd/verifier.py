@@ -128,6 +128,19 @@ class Verifier:
         ([n_nodes] or [n_nodes][n]; outside the vocabulary: NaN and -1) and the top_k alternatives."""
         return abi.tss_get_logprobs(self.ctx, n_nodes, tokens, top_k)
 
+    def beams(self, scores, n, ended=None, end_token=0):
+        """(score, parent, token) [groups][n]: the n best continuations of each group of beams, scores [groups][beams],
+        from the last verify's first groups * beams rows (one-node drafts, a beam each)."""
+        return abi.tss_get_beams(self.ctx, scores, n, ended, end_token)
+
+    def reorder(self, seqs, parents, first=0):
+        """Sequence seqs[i] becomes what seqs[parents[i]] was, all at once; their first `first` tokens are the same."""
+        seqs, parents = abi._int32s(seqs, "seqs"), abi._int32s(parents, "parents")
+        abi.tss_seq_reorder(self.ctx, seqs, parents, first)
+        masks = [self._mask[int(seqs[p])] for p in parents]
+        for s, m in zip(seqs, masks):
+            self._mask[int(s)] = m.copy()
+
     def check_kv(self):
         """Raises if the KV binding is inconsistent (page table, lengths)."""
         abi.tss_check_kv(self.ctx)
