@@ -122,31 +122,35 @@ def _cache(pages, page_table=None):
     return kv
 
 
-def _by_heads(t, name, rows):
-    """Refuses what is not [rows][heads][head_dim] with a row's heads one after the other; the rows' stride."""
-    heads, hd = t.shape[1:]
-    if rows and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != hd) or (rows > 1 and t.stride(0) < heads * hd)):
+def _by_heads(t, name, shape):
+    """Refuses a tensor of this shape [rows][heads][head_dim] whose rows do not hold their heads one after the other; the
+    rows' stride."""
+    rows, heads, hd = shape
+    row, head, one = t.stride()
+    if rows and (one != 1 or (head != hd and heads > 1) or (row < heads * hd and rows > 1)):
         raise ValueError(f"a row of {name} must hold its heads one after the other")
-    return t.stride(0) if rows > 1 else heads * hd
+    return row if rows > 1 else heads * hd
 
 
 def _queries(kv, q, pages, scale, out):
     """Checks of an attention call's q, out and scale: (rows, heads, out, strides of q and out, scale)."""
-    dev, hd = pages.device, kv.head_dim
+    dev = pages.device
     _on_device(q, "q", dev)
-    if q.dim() != 3 or q.dtype != pages.dtype or q.shape[2] != hd or q.shape[1] < 1 or q.shape[1] % kv.n_kv_heads:
+    shape, dtype = q.shape, q.dtype
+    if len(shape) != 3 or dtype != pages.dtype or shape[2] != kv.head_dim or shape[1] < 1 or shape[1] % kv.n_kv_heads:
         raise ValueError("q must be [rows][a multiple of the cache's heads][head_dim] of the cache's type")
-    rows, heads, _ = q.shape
-    out = torch.empty((rows, heads, hd), dtype=q.dtype, device=dev) if out is None else out
-    _on_device(out, "out", dev)
-    if out.shape != q.shape or out.dtype != q.dtype:
-        raise ValueError("out must be like q")
-    q_stride, out_stride = _by_heads(q, "q", rows), _by_heads(out, "out", rows)
+    if out is None:
+        out, out_stride = torch.empty(shape, dtype=dtype, device=dev), shape[1] * shape[2]
+    else:
+        _on_device(out, "out", dev)
+        if out.shape != shape or out.dtype != dtype:
+            raise ValueError("out must be like q")
+        out_stride = _by_heads(out, "out", shape)
     if scale is None:
         scale = 0.0                      # the library's default
     elif ctypes.c_float(scale).value == 0:
         raise ValueError("scale must not be 0 in fp32 (None is 1 / sqrt(head_dim))")
-    return rows, heads, out, q_stride, out_stride, scale
+    return shape[0], shape[1], out, _by_heads(q, "q", shape), out_stride, scale
 
 
 def _sequences(kv, row_offsets, lengths, rows, max_rows, max_length, dev):
@@ -209,26 +213,32 @@ def append_kv(q, k, v, pages, page_table, row_offsets, lengths, positions=None, 
     input.  Rows behind the last sequence and before token 0 are left as they were."""
     kv = _cache(pages, page_table)
     dev, hd = pages.device, kv.head_dim
-    for t, name in ((k, "k"), (v, "v")) + (() if q is None else ((q, "q"),)):
-        _on_device(t, name, dev)
-        if t.dim() != 3 or t.shape[2] != hd or t.dtype not in _TYPES or t.dtype != k.dtype or t.shape[0] != k.shape[0]:
-            raise ValueError("q, k and v must be [rows][heads][head_dim] of one type and number of rows")
-        if name != "q" and t.shape[1] != kv.n_kv_heads:
-            raise ValueError("k and v must have the cache's heads")
-    rows, heads = k.shape[0], 0 if q is None else q.shape[1]
+    _on_device(k, "k", dev)
+    _on_device(v, "v", dev)
+    shape, dtype = k.shape, k.dtype
+    if len(shape) != 3 or shape[1] != kv.n_kv_heads or shape[2] != hd or dtype not in _TYPES or v.shape != shape \
+            or v.dtype != dtype:
+        raise ValueError("k and v must be [rows][the cache's heads][head_dim] of one type")
+    rows, heads = shape[0], 0
     q_at = q_out = None
     q_stride = out_stride = 0
-    if heads:
-        out = torch.empty(q.shape, dtype=pages.dtype, device=dev) if out is None else out
-        _on_device(out, "out", dev)
-        if out.shape != q.shape or out.dtype != pages.dtype:
-            raise ValueError("out must be like q, of the cache's type")
-        q_at, q_out = q.data_ptr(), out.data_ptr()
-        q_stride, out_stride = _by_heads(q, "q", rows), _by_heads(out, "out", rows)
-    elif q is not None:
-        out = torch.empty(q.shape, dtype=pages.dtype, device=dev) if out is None else out
-    else:
+    if q is None:
         out = None
+    else:
+        _on_device(q, "q", dev)
+        q_shape = q.shape
+        if len(q_shape) != 3 or q_shape[0] != rows or q_shape[2] != hd or q.dtype != dtype:
+            raise ValueError("q must be [rows][heads][head_dim] of k's type and number of rows")
+        heads = q_shape[1]
+        if out is None:
+            out, out_stride = torch.empty(q_shape, dtype=pages.dtype, device=dev), heads * hd
+        else:
+            _on_device(out, "out", dev)
+            if out.shape != q_shape or out.dtype != pages.dtype:
+                raise ValueError("out must be like q, of the cache's type")
+            out_stride = _by_heads(out, "out", q_shape)
+        if heads:
+            q_at, q_out, q_stride = q.data_ptr(), out.data_ptr(), _by_heads(q, "q", q_shape)
     offs, lens, max_rows, _ = _sequences(kv, row_offsets, lengths, rows, max_rows, None, dev)
     pos = None if positions is None else _indices(positions, "positions", (rows,), dev)
     if rope is None:
@@ -243,8 +253,8 @@ def append_kv(q, k, v, pages, page_table, row_offsets, lengths, positions=None, 
         if len(freq) != hd // 2:
             raise ValueError("rope must have head_dim / 2 frequencies")
         freq = (ctypes.c_double * len(freq))(*freq)
-    _call(dev, abi.tss_append_kv, kv, layer, q_at, q_stride, heads, k.data_ptr(), _by_heads(k, "k", rows), v.data_ptr(),
-          _by_heads(v, "v", rows), _TYPES[k.dtype], offs, lens, pos, rows, max_rows, freq, q_out, out_stride)
+    _call(dev, abi.tss_append_kv, kv, layer, q_at, q_stride, heads, k.data_ptr(), _by_heads(k, "k", shape), v.data_ptr(),
+          _by_heads(v, "v", shape), _TYPES[dtype], offs, lens, pos, rows, max_rows, freq, q_out, out_stride)
     return out
 
 
