@@ -160,7 +160,7 @@ struct PickShared {
   int at[kPickList];
   int holder[kPickHolders];
   int part[kPickList];
-  double best[kPickWaves];
+  float top[kPickWaves];
   unsigned cut[kPickWaves], have[kPickWaves];
   float near[kPickThreads], far;
   int n_near;
@@ -222,22 +222,22 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a, BeamPart
     int b = i / per;
     if (s.state[b] == 1) mine = fmax(mine, value(b, grain(i, b)));
   }
-  double best = mine;
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) best = fmax(best, __shfl_xor(best, off));
-  if (lane == 0) {
-    s.best[wave] = best;
-    s.have[wave] = 0;
-  }
+  // a little above the best of all
+  const float wave_top = wave_max((float)mine);
   const unsigned have = __popcll(__ballot(mine > -INFINITY));
-  if (lane == 0) s.have[wave] = have;
+  if (lane == 0) {
+    s.top[wave] = wave_top;
+    s.have[wave] = have;
+  }
   __syncthreads();
-  unsigned all = 0;
+  float top = s.top[0];
+  unsigned all = s.have[0];
 #pragma unroll
-  for (int w = 0; w < kPickWaves; ++w) {
-    best = fmax(best, s.best[w]);
+  for (int w = 1; w < kPickWaves; ++w) {
+    top = fmaxf(top, s.top[w]);
     all += s.have[w];
   }
+  const double best = nextafterf(top, INFINITY);
   // a first cut, as a distance behind the best in fp32 (its 16 upper bits): the need-th of a
   // wave's threads, which has its share of those with candidates
   const unsigned key = mine > -INFINITY ? __float_as_uint((float)(best - mine)) >> 16 : 0xffffu;
