@@ -650,10 +650,6 @@ __device__ __forceinline__ void rows_block(const A& a, const Place& w, const Blo
         for (int t = 0; t < TILES; ++t) S[t][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[t][c], S[t][p], 0, 0, 0);
       }
     }
-    // The next step's loads go out behind these products: in front of them the wave waited for the
-    // loads' queue and, while they landed, for its reads of K (a step of 128 rows 4560 cycles,
-    // now 3740).
-    if (st + 1 < n_st) issue(st + 1);
     // V is requested before the softmax, whose instructions hide it; the empty asm
     // keeps the compiler from moving the reads down to their use.  Two pages' tokens of a dimension beside each other, as the product takes them, in reads
     // of 8 bytes: read 16 at a time they would have to be moved, 48 moves a step.  Volatile, for
@@ -671,6 +667,10 @@ __device__ __forceinline__ void rows_block(const A& a, const Place& w, const Blo
           const f16x4 x = *(const volatile LdsHalfs*)at, y = *(const volatile LdsHalfs*)(at + 2 * NK * 1024);
           V[h][i][e] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
         }
+    // The next step's loads go out behind the reads of K and V: in front of them the wave waited for
+    // the loads' queue and, while they landed, for LDS (a step of 128 rows alone on a CU 4560 cycles,
+    // behind K's reads 3740; 2048 rows of 32 heads 65 us, behind K's 59.5, behind V's too 58).
+    if (st + 1 < n_st) issue(st + 1);
     asm volatile("" ::: "memory");
     const bool whole = i1 <= span.all_last && (i1 < full_sinks || i0 >= span.all_first);
     if (EDGE || !whole) {
