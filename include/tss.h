@@ -552,7 +552,7 @@ int tss_copy_pages(void* hip_stream, const tss_paged_kv* kv, const int32_t* src,
  *     its slot.  Any int32 is one.
  *   inv_freq: host, head_dim / 2 frequencies f_j: dimensions j and j + head_dim / 2
  *     turn by position * f_j, base^(-2j / head_dim) for LLaMA; NULL: no rotation.
- *     They must be finite.  Angles are formed in 64 bits.
+ *     They must be at most 1e6 in size.  Angles are formed in 64 bits.
  *   q_out: [rows][n_q_heads][head_dim] of the cache's type; may be q (of that type, with
  *     its stride), otherwise it shares no element with an input.
  *   max_rows: upper bound of a sequence's rows; rows beyond it are not taken.

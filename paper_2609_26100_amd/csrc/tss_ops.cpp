@@ -256,7 +256,8 @@ int tss_append_kv(void* hip_stream, const tss_paged_kv* kv, int32_t layer, const
   if (inv_freq) {
     a.rotate = 1;
     for (int j = 0; j < kv->head_dim / 2; ++j) {
-      if (!std::isfinite(inv_freq[j])) return refuse(TSS_EINVAL, me, "a frequency is not finite");
+      // at a million radians a position, 2^31 positions leave 64 bits no fraction of a turn to speak of
+      if (!(std::fabs(inv_freq[j]) <= 1e6)) return refuse(TSS_EINVAL, me, "a frequency is beyond 1e6 in size");
       a.turns[j] = inv_freq[j] / 6.283185307179586476925;
     }
   }

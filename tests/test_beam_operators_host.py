@@ -58,6 +58,7 @@ def refused(call, status, name, *args, **kw):
     dict(n_q_heads=-1), dict(n_q_heads=65536), dict(rows=-1), dict(max_rows=-1), dict(q=None), dict(k=None),
     dict(v=None), dict(q_out=None), dict(row_offsets=None), dict(lengths=None), dict(q=P + 8), dict(k=P + 4),
     dict(v=P + 2), dict(q_out=P + 8), dict(inv_freq=(ctypes.c_double * 64)(*[float("inf")] * 64)),
+    dict(inv_freq=(ctypes.c_double * 64)(*[-1.1e6] * 64)),
     dict(inv_freq=(ctypes.c_double * 64)(*([1.0] * 31 + [float("nan")] + [1.0] * 32)))])
 def test_append_refuses(bad):
     refused(append, abi.TSS_EINVAL, "tss_append_kv", **bad)

@@ -166,6 +166,18 @@ def test_values_beyond_fp16_and_special():
     assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got[~got.isnan()], want[~want.isnan()])
 
 
+def test_beyond_four_gib():
+    c = Case([64], [40], 2, 8, 128, "bf16", "f16", seed=11)
+    want_pool, want = c.run()
+    pool = torch.zeros(1, 70000, 2, 8, 16 * 128, dtype=torch.float16, device=DEV)      # 4.6 GB
+    where = torch.tensor([[69999, 3, 69000, 40000]], dtype=torch.int32)
+    pool[0, where[0].long()] = c.pool[0, c.table[0].long()].to(DEV)
+    small, c.pool, c.table = c.table[0].long(), pool, where
+    got_pool, got = c.run()
+    assert torch.equal(bits(got), bits(want))
+    assert torch.equal(bits(got_pool[0, where[0].long()]), bits(want_pool[0, small]))
+
+
 def test_captured_and_replayed():
     c = Case([50, 33], [5, 3], 4, 2, 128, "bf16", "f16", seed=9, behind=0)
     pool, qkv = c.pool.to(DEV), c.qkv.to(DEV)

@@ -117,6 +117,7 @@ CASES = [
     ([(40, [645] * 30)], [5] * 30, 1, 1, 64),
     ([(63, [1009 + i for i in range(12)])], [1] * 12, 3, 4, 128),
     ([(200, [3300, 3201])], [1, 1], 1, 1, 64),
+    ([(2, [33 + i for i in range(70)])], [1] * 70, 1, 2, 64),            # more sequences than a wave has lanes
 ]
 
 
@@ -196,6 +197,20 @@ def test_scale_strides_layers_and_rows_behind():
         got = run(c, [1, 2], view, scale=scale, out=view)
         assert got.data_ptr() == view.data_ptr() and not view[3:].any()
         compare(got[:3], q, [1, 2], c, scale)
+
+
+def test_beyond_four_gib():
+    """Page ids whose bytes lie beyond 4 GiB, shared and own."""
+    c = Groups([(3, [60, 49, 70])], 8, 128, "f16", 13, lone=False)
+    q = queries([2, 1, 1], 16, 128, "f16", 13)
+    want = run(c, [2, 1, 1], q)
+    n = c.pool.shape[1]
+    at = torch.randperm(n, generator=torch.Generator().manual_seed(1)) * (70000 // n)
+    at[0] = 69999
+    pool = torch.zeros(1, 70000, 2, 8, 16 * 128, dtype=torch.float16, device=DEV)          # 4.6 GB
+    pool[0, at.to(DEV)] = c.pool[0].to(DEV)
+    c.pool, c.table = pool, torch.where(c.table >= 0, at[c.table.long().clamp_min(0)].int(), -1)
+    assert torch.equal(run(c, [2, 1, 1], q), want)
 
 
 def test_special_values():
