@@ -19,14 +19,15 @@
 // streams pages of its own into registers and the waves' states meet at the end;
 // many rows share each page through LDS, a wave for each 16 or 32 rows.  Where
 // the blocks are too few for the chip, each block's pages are split among several
-// workgroups and a second launch joins their states.
+// workgroups and a second launch joins their states.  The blocks stand in window_core.h.
 //
 // Long contexts of few rows are bound by HBM (5 rows of 32 heads over 8 kv heads
-// and 100003 tokens, 410 MB: 74 + 5 us, 5.2 TB/s), short ones by their two launches
-// (one row of 32 heads over 1028 tokens 8.9 + 3.1 us).  Blocks of many rows take, for
+// and 100003 tokens, 410 MB: 72 + 5 us, 5.3 TB/s), short ones by their two launches
+// (one row of 32 heads over 1028 tokens 8.4 + 3.1 us).  Blocks of many rows take, for
 // each step of 64 tokens and 128 rows, 0.43 us each of a SIMD's matrix products and of
 // its LDS reads and as much of the softmax, and two waves a SIMD hide little of one
-// behind the other (2048 rows of 32 heads, 1028 tokens each: 57 us, 600 TFLOP/s).
+// behind the other (2048 rows of 32 heads, 1028 tokens each: 58 us, 590 TFLOP/s, in the
+// same trace as the 65 of loads before the products).
 //
 // Of an fp16 cache, the probabilities go to fp16 for the second product (two terms each
 // would take twice its instructions): outputs are off by 2.3e-4 to 2.9e-4 of their size

@@ -651,9 +651,10 @@ __device__ __forceinline__ void rows_block(const A& a, const Place& w, const Blo
       }
     }
     // V is requested before the softmax, whose instructions hide it; the empty asm
-    // keeps the compiler from moving the reads down to their use.  Two pages' tokens of a dimension beside each other, as the product takes them, in reads
-    // of 8 bytes: read 16 at a time they would have to be moved, 48 moves a step.  Volatile, for
-    // the compiler joins reads otherwise.
+    // keeps the compiler from moving the reads down to their use.  Two pages' tokens of a
+    // dimension beside each other, as the product takes them, in reads of 8 bytes: read 16
+    // at a time they would have to be moved, 48 moves a step.  Volatile, for the compiler
+    // joins reads otherwise.
     typedef __attribute__((address_space(3))) uint8_t Lds;
     typedef __attribute__((address_space(3))) f16x4 LdsHalfs;
     f16x8 V[kRowsPages / 2][NK][2];
