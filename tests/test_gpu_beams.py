@@ -119,6 +119,27 @@ def test_far_values(kind):
     check(x, torch.tensor([[-1.0, -2.0]]), 8)
 
 
+@pytest.mark.parametrize("vocab", [300, 40000])
+def test_scores_at_the_ends_of_fp32(vocab):
+    """Scores beside which a token's log probability is nothing even in 64 bits: a beam's tokens are all equal."""
+    big = torch.finfo(torch.float32).max
+    for scores in ([big, big, -1.0], [-1.0, big, -big], [-big, -big, -big], [0.0, 1e-45, -1e-45]):
+        x, _ = make(1, 3, vocab, "f32", 9)
+        check(x, torch.tensor([scores]), 20)
+    check(torch.zeros(4, 1), torch.tensor([[3e-45, 1e-44, 0.0, -1e-45]]), 4)     # values of a few smallest steps
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_largest_vocabulary(kind):
+    x, scores = make(2, 2, 1 << 20, kind, 10)
+    x[0, -1] = x[0].max() + 1
+    r = check(x, scores, 64)
+    assert r.token[0, 0] == (1 << 20) - 1
+    x[:] = 0.0                                       # every candidate of a beam equal: ordered by token
+    r = check(x, torch.tensor([[-1.0, -2.0], [-2.0, -1.0]]), 64)
+    assert r.token.tolist() == [list(range(64))] * 2 and r.parent[:, 0].tolist() == [0, 1]
+
+
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("skew,pad", [(0, 1), (1, 0), (3, 5), (7, 2)])
 def test_rows_that_are_not_aligned(kind, skew, pad):

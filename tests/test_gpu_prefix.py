@@ -222,6 +222,62 @@ def test_special_values():
 
 
 @pytest.mark.parametrize("kind", ["f16", "f32"])
+@pytest.mark.parametrize("seqs", [1, 40, 128])          # blocks of 16, 64 and 128 rows
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("size", [30.0, 300.0, 3e3, 3e4])
+def test_scores_far_from_zero(kind, seqs, sign, size):
+    """Equal scores of any finite size, in shared and own pages: the mean of V, as at zero.  Up to 6e10 times 1 / 8."""
+    shared, heads, hd = 14, 2, 64
+    c = Groups([(shared, [16 * shared + 1 + i % 21 for i in range(seqs)])], heads, hd, kind, 14)
+    for k, v in c.kv:
+        k[:] = sign * size
+    ids = c.table[c.table >= 0].unique().long()
+    c.pool[0, ids, 0] = torch.where(c.pool[0, ids, 0].isnan(), torch.nan, sign * size).to(c.pool.dtype)
+    q = torch.full((seqs, heads, hd), size, dtype=TYPES[kind])
+    got = run(c, [1] * seqs, q).double().cpu()
+    half = ref.HALF if kind == "f16" else ref.F32
+    for i in range(seqs):
+        v = c.kv[i][1].double()
+        n, want = v.shape[0], v.mean(0)
+        # equal weights (powers of two, exact), sums of n terms in fp32 and the roundings of 1 / L and of the result
+        bound = n * ref.F32 * v.abs().mean(0) * 2 + (half + 2 * ref.F32) * want.abs() + 2.0 ** -25
+        assert ((got[i] - want).abs() <= bound).all(), (i, float((got[i] - want).abs().max()))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("seqs", [2, 130, 256])         # blocks of 16, 64 and 128 rows, the last two of more than 64 pages
+def test_many_small_weights_beside_a_dominant_one(seqs, hd):
+    """A first shared token with nearly all of the weight, e^-18 of it for 20000 shared and a few own tokens each."""
+    shared, heads = 1250, 16
+    n = 16 * shared
+    g = torch.Generator().manual_seed(hd + 1)
+    k, v = torch.zeros(n + seqs * 3, heads, hd), 4 + torch.randn(n + seqs * 3, heads, hd, generator=g)
+    k[0, :, 0] = 18.0
+    v[0] = 0
+    k, v = k.half(), v.half()
+    own = [n + 3 * i for i in range(seqs)]                # three own tokens each, of which 1 + i % 3 are there
+    lens = [n + 1 + i % 3 for i in range(seqs)]
+    pages = torch.cat([ops.pack_pages(k[:n], v[:n])] + [ops.pack_pages(k[o:o + 3], v[o:o + 3]) for o in own])[None].to(DEV)
+    table = torch.arange(shared + 1, dtype=torch.int32).repeat(seqs, 1)
+    table[:, shared] = shared + torch.arange(seqs)
+    q = torch.zeros(seqs, heads, hd)
+    q[:, :, 0] = hd ** 0.5
+    q = q.half()
+    got = ops.prefix_attention(q.to(DEV), pages, table.to(DEV), offsets([1] * seqs), ints(lens), ints([shared]),
+                               max_rows=1).double().cpu()
+    for r, h in ((0, 0), (seqs - 1, heads - 1), (seqs // 2, 5)):
+        m = lens[r] - n
+        kr, vr = (torch.cat([x[:n, h], x[own[r]:own[r] + m, h]]).double() for x in (k, v))
+        p = torch.softmax(q[r, h].double() @ kr.T / hd ** 0.5, 0)
+        want, pv, big = p @ vr, p @ vr.abs(), float(vr.abs().max())
+        # a weight's rounding in fp16 is at most 2^-32 of the largest: the scores are exact (one product of two fp16
+        # values and a power of two or 1 / sqrt(128)), 18 log2 e and its exponent round; sums of n terms in fp32
+        bound = 2 * (18 + 8) * 6 * ref.F32 * pv + 2 * n * ref.F32 * pv + ref.HALF * pv + n * 2.0 ** -32 * big \
+            + ref.HALF * want.abs() + 2.0 ** -25
+        assert ((got[r, h] - want).abs() <= bound).all(), (r, h, float(((got[r, h] - want).abs() / bound).max()))
+
+
+@pytest.mark.parametrize("kind", ["f16", "f32"])
 def test_equal_runs(kind):
     c = Groups([(30, [500, 520, 481]), (12, [200])], 2, 128, kind, 8)
     rows = [3, 1, 2, 9]
