@@ -150,6 +150,22 @@ def test_rows_that_are_not_aligned(kind, skew, pad):
     check(x, scores, 6, dev=dev)
 
 
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("skew,vocab,pad", [(0, 3001, 0), (0, 50021, 0), (3, 5001, 2), (1, 32001, 1), (5, 9000, 7),
+                                            (2, 7, 0), (1, 2048, 3)])
+def test_ties_of_rows_at_other_places_of_their_blocks(skew, vocab, pad, kind):
+    """Equal rows have equal candidates wherever they begin: the order of ties is by beam, then by token."""
+    x, _ = make(1, 1, vocab, kind, vocab + pad)
+    x = x.repeat(8, 1)
+    buf = torch.full((8 * (vocab + pad) + skew,), torch.nan, dtype=x.dtype, device=DEV)
+    dev = buf[skew:].view(8, vocab + pad)[:, :vocab]
+    dev.copy_(x)
+    n = min(32, 4 * vocab)
+    r = check(x, torch.full((1, 8), -2.5), n, dev=dev)
+    want = ops.beam_select(x.to(DEV).contiguous(), torch.full((1, 8), -2.5, device=DEV), n)
+    assert all(torch.equal(a, b) for a, b in zip(r, want))
+
+
 def test_beyond_four_gib():
     rows, vocab = 40, 60_000_000 // 64                # rows 240 MB apart
     buf = torch.full((rows, 60_000_000), -100.0, dtype=torch.float32, device=DEV)
