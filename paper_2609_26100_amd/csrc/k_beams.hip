@@ -7,12 +7,14 @@
 // (in the logits' type, so exactly; 3 % of the bytes read).  Waves meet nowhere.
 //
 // The second has a workgroup for each group.  It joins the rows' sums and finds a cut that
-// at least n candidates reach: every thread has the best of its share of the parts (of the
-// lanes, where parts are few), and the n-th best thread is the cut (found among those that
-// reach the lowest of the waves' own cuts, a bisection over ballots each).  Then it opens
-// what reaches the cut, parts, lanes, logits, and the few candidates found (38 for n = 32)
-// are ordered by counting how many precede each.  Where too many are equal for the lists,
-// the cut is searched for bit by bit over all logits of the group.
+// at least n candidates reach: every thread has the best of its share of the parts of the beams
+// that can win (of their lanes, where parts are few), and the n-th best thread is the cut (found
+// among those that reach the lowest of the waves' own cuts, a bisection over ballots each).
+// Then it opens what reaches the cut, parts, lanes, logits, and the few candidates found (38
+// for n = 32) are ordered by counting how many precede each.  Where the best candidates are in
+// few of the parts, a second cut is found among the lanes of the parts that reach the first.
+// Where too many are equal for the lists, the cut is searched for bit by bit over all logits of
+// the group (16 beams of 32000 equal logits 1.3 ms).
 //
 // Bound by HBM where there is much to read (32 groups of 16 beams of 131072 bf16 logits, 134 MB:
 // the first launch 24 us, 5.6 TB/s; the second 14, on 32 CUs), else by the dependent
@@ -36,6 +38,15 @@ constexpr int kBeamWaves = 4;                    // parts of a workgroup
 constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64;
 constexpr int kPickList = 1024;                  // candidates, opened parts
 constexpr int kPickHolders = 2048;               // opened lanes
+// Parts that beams must have for each candidate, else their lanes are looked through at once.  With
+// 1 one of 32 beams of 131072 tokens, n = 64, takes 34.5 us a call in a graph, with 2 and 4 27.9;
+// with 4 one of 16 beams of 200000, n = 32, 27.2, with 1 and 2 23.0.
+constexpr int kPickParts = 2;
+// Lanes that reach the parts' cut beyond which another is found.  With 512, four beams of 32000 masked
+// down to 1500 tokens each take 97 us, with 256 21; with 1024, 32 beams of 20000 whose scores are 1.5
+// apart 351, with 256 and 512 34.
+constexpr int kPickMany = 256;
+constexpr double kNoCut = -1.7976931348623157e308;  // every candidate reaches it
 constexpr double kLog2eD = 1.4426950408889634074;
 constexpr float kLog2eHi = (float)kLog2eD, kLog2eLo = (float)(kLog2eD - (double)kLog2eHi);
 
@@ -159,6 +170,7 @@ __device__ __forceinline__ double weighed(double S, float m, float to) {
 struct PickShared {
   double m[TSS_BEAMS_MAX], c[TSS_BEAMS_MAX];  // of the beams: NaN c, no candidates
   int state[TSS_BEAMS_MAX];                   // 0: lost, 1: alive, 2: ended
+  int beam[TSS_BEAMS_MAX];                    // those alive
   double v[kPickList];
   int at[kPickList];
   int holder[kPickHolders];
@@ -178,7 +190,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a, BeamPart
   const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, B = a.n_beams, V = a.vocab;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row0 = g * B;
-  if (tid == 0) s.n = s.n_near = s.holders = s.parts = 0;
+  if (tid == 0) s.n = s.holders = s.parts = 0;
   // the rows' sums, a wave each
   for (int b = wave; b < B; b += kPickWaves) {
     const size_t at = (size_t)(row0 + b) * parts;
@@ -210,71 +222,6 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a, BeamPart
   }
   __syncthreads();
   auto value = [&](int b, float x) { return (double)x - s.m[b] + s.c[b]; };
-  // where a group has few parts, the lanes' largest logits are looked through at once
-  const bool by_parts = B * parts >= 4 * a.n;
-  const int per = by_parts ? parts : parts * 64, count = B * per;
-  auto grain = [&](int i, int& b) {
-    b = i / per;
-    const size_t at = (size_t)row0 * per + i;
-    return by_parts ? p.tops[at] : L::at(p.lanes, at);
-  };
-  // neighbours in the list go to different waves, so that every wave has some of every beam and
-  // its cut is about the group's
-  double mine = -INFINITY;
-  for (int i = lane * kPickWaves + wave; i < count; i += kPickThreads) {
-    int b = i / per;
-    if (s.state[b] == 1) mine = fmax(mine, value(b, grain(i, b)));
-  }
-  // a little above the best of all
-  const float wave_top = wave_max((float)mine);
-  const unsigned have = __popcll(__ballot(mine > -INFINITY));
-  if (lane == 0) {
-    s.top[wave] = wave_top;
-    s.have[wave] = have;
-  }
-  __syncthreads();
-  float top = s.top[0];
-  unsigned all = s.have[0];
-#pragma unroll
-  for (int w = 1; w < kPickWaves; ++w) {
-    top = fmaxf(top, s.top[w]);
-    all += s.have[w];
-  }
-  const double best = nextafterf(top, INFINITY);
-  // a first cut, as a distance behind the best in fp32 (its 16 upper bits): the need-th of a
-  // wave's threads, which has its share of those with candidates
-  const unsigned key = mine > -INFINITY ? __float_as_uint((float)(best - mine)) >> 16 : 0xffffu;
-  const unsigned need = all >= (unsigned)a.n ? (have * a.n + all - 1) / all : have;
-  unsigned cut = 0;  // most keys below it: fewer than need
-#pragma unroll
-  for (int bit = 15; bit >= 0; --bit) {
-    const unsigned c = cut | (1u << bit);
-    cut = (unsigned)__popcll(__ballot(key < c)) < need ? c : cut;
-  }
-  if (lane == 0) s.cut[wave] = need ? cut : 0;
-  __syncthreads();
-  cut = 0;
-#pragma unroll
-  for (int w = 0; w < kPickWaves; ++w) cut = max(cut, s.cut[w]);
-  // of the threads that reach it (few more than n, for the waves differ), the n-th best is the
-  // cut; a distance in fp32 is off by half a step
-  double least = -INFINITY;
-  if (all >= (unsigned)a.n) {
-    if (key <= cut) s.near[atomicAdd(&s.n_near, 1)] = (float)(best - mine);
-    __syncthreads();
-    const int c = s.n_near;
-    for (int i = tid >> 2; i < (c + 15) / 16 * 16; i += kPickThreads / 4) {
-      const float d = s.near[min(i, c - 1)];
-      int place = 0;
-      for (int j = tid & 3; j < c; j += 4) place += s.near[j] < d || (s.near[j] == d && j < i);
-      place += __shfl_xor(place, 1);
-      place += __shfl_xor(place, 2);
-      if (i < c && place == a.n - 1) s.far = d;
-    }
-    __syncthreads();
-    least = s.far < INFINITY ? best - (double)s.far * (1 + 1e-7) : -INFINITY;
-  }
-  const double lowest = least == -INFINITY ? -1.7976931348623157e308 : least;
   auto list = [&](double v, int at) {
     const int i = atomicAdd(&s.n, 1);
     if (i < kPickList) {
@@ -282,32 +229,135 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a, BeamPart
       s.at[i] = at;
     }
   };
-  if (tid < B && s.state[tid] == 2) list(s.c[tid], tid * V + a.end_token);
   auto hold = [&](int id) {
     const int i = atomicAdd(&s.holders, 1);
     if (i < kPickHolders) s.holder[i] = id;
   };
-  for (int i = lane * kPickWaves + wave; i < count; i += kPickThreads) {
-    int b = i / per;
-    if (s.state[b] != 1) continue;
-    if ((count <= kPickThreads ? mine : value(b, grain(i, b))) >= lowest) {
-      if (by_parts) {
-        const int k = atomicAdd(&s.parts, 1);
-        if (k < kPickList) s.part[k] = i;
-      } else {
-        hold(i);
+  // a value that the n-th best of the threads' own reaches, so that at least n candidates do
+  // (the lowest finite one, where fewer threads have a candidate)
+  auto cut_of = [&](double mine) {
+    // a little above the best of all
+    const float wave_top = wave_max((float)mine);
+    const unsigned have = __popcll(__ballot(mine > -INFINITY));
+    if (lane == 0) {
+      s.top[wave] = wave_top;
+      s.have[wave] = have;
+    }
+    if (tid == 0) s.n_near = 0;
+    __syncthreads();
+    float top = s.top[0];
+    unsigned all = s.have[0];
+#pragma unroll
+    for (int w = 1; w < kPickWaves; ++w) {
+      top = fmaxf(top, s.top[w]);
+      all += s.have[w];
+    }
+    const double best = nextafterf(top, INFINITY);
+    // a first cut, as a distance behind the best in fp32 (its 16 upper bits): the need-th of a
+    // wave's threads, which has its share of those with candidates
+    const unsigned key = mine > -INFINITY ? __float_as_uint((float)(best - mine)) >> 16 : 0xffffu;
+    const unsigned need = all >= (unsigned)a.n ? (have * a.n + all - 1) / all : have;
+    unsigned cut = 0;  // most keys below it: fewer than need
+#pragma unroll
+    for (int bit = 15; bit >= 0; --bit) {
+      const unsigned c = cut | (1u << bit);
+      cut = (unsigned)__popcll(__ballot(key < c)) < need ? c : cut;
+    }
+    if (lane == 0) s.cut[wave] = need ? cut : 0;
+    __syncthreads();
+    cut = 0;
+#pragma unroll
+    for (int w = 0; w < kPickWaves; ++w) cut = max(cut, s.cut[w]);
+    // of the threads that reach it (few more than n, for the waves differ), the n-th best is the
+    // cut; a distance in fp32 is off by half a step
+    double least = -INFINITY;
+    if (all >= (unsigned)a.n) {
+      if (key <= cut) s.near[atomicAdd(&s.n_near, 1)] = (float)(best - mine);
+      __syncthreads();
+      const int c = s.n_near;
+      for (int i = tid >> 2; i < (c + 15) / 16 * 16; i += kPickThreads / 4) {
+        const float d = s.near[min(i, c - 1)];
+        int place = 0;
+        for (int j = tid & 3; j < c; j += 4) place += s.near[j] < d || (s.near[j] == d && j < i);
+        place += __shfl_xor(place, 1);
+        place += __shfl_xor(place, 2);
+        if (i < c && place == a.n - 1) s.far = d;
       }
+      __syncthreads();
+      least = s.far < INFINITY ? best - (double)s.far * (1 + 1e-7) : -INFINITY;
     }
-  }
-  __syncthreads();
-  if (by_parts && s.parts <= kPickList) {
-    for (int i = tid; i < s.parts * 64; i += kPickThreads) {
-      const int id = s.part[i / 64] * 64 + i % 64, b = s.part[i / 64] / parts;
-      if (value(b, L::at(p.lanes, (size_t)row0 * parts * 64 + id)) >= lowest) hold(id);
-    }
+    return least == -INFINITY ? kNoCut : least;
+  };
+  // f(i) for this thread's share of 0 .. count - 1: neighbours go to different waves, so that every
+  // wave has some of every beam and its cut is about the group's
+  auto share = [&](int count, auto f) {
+    for (int i = lane * kPickWaves + wave; i < count; i += kPickThreads) f(i);
+  };
+  // the beams that can win; lost and ended ones have nothing to look through
+  const bool wins = lane < B && s.state[min(lane, B - 1)] == 1;
+  const u64 winners = __ballot(wins);
+  const int alive = __popcll(winners);
+  if (alive < B) {
+    if (wave == 0 && wins) s.beam[__popcll(winners & ((1ull << lane) - 1))] = lane;
     __syncthreads();
   }
-  bool fits = s.parts <= kPickList && s.holders <= kPickHolders;
+  const bool by_parts = alive * parts >= kPickParts * a.n;
+  const int per = by_parts ? parts : parts * 64, count = alive * per;
+  auto place = [&](int i, int& b) {  // of part or lane i of these beams
+    const int k = i / per;
+    b = alive < B ? s.beam[k] : k;
+    return i + (b - k) * per;
+  };
+  auto lane_top = [&](int b, int id) { return value(b, L::at(p.lanes, (size_t)row0 * parts * 64 + id)); };
+  auto grain = [&](int b, int id) { return by_parts ? value(b, p.tops[(size_t)row0 * parts + id]) : lane_top(b, id); };
+  auto lanes = [&](auto f) {  // f(place, value) for the lanes of the parts found
+    share(s.parts * 64, [&](int i) {
+      const int part = s.part[i / 64], id = part * 64 + i % 64;
+      f(id, lane_top(part / parts, id));
+    });
+  };
+  double lowest = kNoCut;
+  bool fits;
+  for (int again = 0;; again = 1) {
+    double mine = -INFINITY;
+    if (again) {
+      lanes([&](int, double v) { mine = fmax(mine, v); });
+    } else {
+      share(count, [&](int i) {
+        int b;
+        const int id = place(i, b);
+        mine = fmax(mine, grain(b, id));
+      });
+    }
+    lowest = fmax(lowest, cut_of(mine));
+    if (again) {
+      if (tid == 0) s.holders = 0;
+    } else {
+      if (tid < B && s.state[tid] == 2) list(s.c[tid], tid * V + a.end_token);
+      share(count, [&](int i) {
+        int b;
+        const int id = place(i, b);
+        if (!((count <= kPickThreads ? mine : grain(b, id)) >= lowest)) return;
+        if (by_parts) {
+          const int k = atomicAdd(&s.parts, 1);
+          if (k < kPickList) s.part[k] = id;
+        } else {
+          hold(id);
+        }
+      });
+    }
+    __syncthreads();
+    fits = s.parts <= kPickList;
+    if (!by_parts || !fits) break;
+    lanes([&](int id, double v) {
+      if (v >= lowest) hold(id);
+    });
+    __syncthreads();
+    // where many lanes reach the parts' cut (or there was none), the best candidates are in few of the
+    // parts (scores far apart, masked logits): it is sought again, among their lanes
+    if (again || s.holders <= (lowest == kNoCut ? kPickList / kBeamVals : kPickMany)) break;
+  }
+  fits = fits && s.holders <= kPickHolders;
   if (fits) {
     for (int i = tid; i < s.holders * kBeamVals; i += kPickThreads) {
       const int id = s.holder[i / kBeamVals], b = id / (parts * 64);

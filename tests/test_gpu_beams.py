@@ -50,6 +50,70 @@ def test_first_step(kind):
     assert (r.parent == 0).all()
 
 
+def few_left(beams, vocab, kind, which):
+    """Beams few of which can go on, or whose best candidates lie in few places: (x, scores, ended)."""
+    x, scores = make(2, beams, vocab, kind, beams + vocab)
+    ended = None
+    if which == "first":
+        scores[:, 0], scores[:, 1:] = 0.0, -torch.inf
+    elif which == "last":
+        scores[:, :-1] = torch.nan
+    elif which == "ended":
+        ended = torch.ones(2, beams, dtype=torch.int32)
+        ended[0, beams // 2] = ended[1, 0] = ended[1, 1] = 0
+    elif which == "apart":
+        scores[:] = -1.5 * torch.arange(beams)
+    elif which == "masked":                          # one stretch of the tokens, in another place for each beam
+        for b in range(2 * beams):
+            at = (b * 777) % (vocab - 1500)
+            x[b, :at], x[b, at + 1500:] = -torch.inf, -torch.inf
+    return x, scores, ended
+
+
+FEW = ["first", "last", "ended", "apart", "masked"]
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("beams,vocab,n", [(16, 32000, 32), (10, 32000, 20), (8, 10000, 8), (32, 20000, 64),
+                                           (3, 50021, 64), (32, 2049, 64)])
+@pytest.mark.parametrize("which", FEW)
+def test_few_beams_that_can_go_on(which, beams, vocab, n, kind):
+    x, scores, ended = few_left(beams, vocab, kind, which)
+    check(x, scores, n, ended, 5)
+
+
+def replays_us(f, n=20):
+    f()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        f()
+    times = []
+    for _ in range(7):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        graph.replay()
+        a.record()
+        for _ in range(n):
+            graph.replay()
+        b.record()
+        torch.cuda.synchronize()
+        times.append(a.elapsed_time(b) * 1000 / n)
+    return min(times)
+
+
+@pytest.mark.parametrize("which", FEW)
+@pytest.mark.parametrize("beams,vocab,n", [(16, 32000, 32), (8, 10000, 8), (32, 20000, 64)])
+def test_few_beams_take_no_search_over_all_logits(beams, vocab, n, which):
+    """The search bit by bit, one workgroup's over every logit several times, is for logits too many of which are equal:
+    it takes 2.5 to 15 times as long as a step of beams that all go on, the other ways less than twice."""
+    x, scores = make(2, beams, vocab, "f32", 1)
+    x, scores = x.to(DEV), (0.1 * scores).to(DEV)
+    usual = replays_us(lambda: ops.beam_select(x, scores, n))
+    y, few, ended = few_left(beams, vocab, "f32", which)
+    y, few, ended = y.to(DEV), few.to(DEV), None if ended is None else ended.to(DEV)
+    assert replays_us(lambda: ops.beam_select(y, few, n, ended, 5)) < 2 * usual
+
+
 def test_ended_beams():
     x, scores = make(4, 5, 700, "f32", 2)
     ended = torch.tensor([[1, 0, 0, 0, 1], [0, 0, 0, 0, 0], [1, 1, 1, 1, 1], [0, 1, 0, 9, -1]], dtype=torch.int32)
