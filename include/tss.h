@@ -578,7 +578,8 @@ int tss_append_kv(void* hip_stream, const tss_paged_kv* kv, int32_t layer, const
  *     with n_groups 1: every sequence.
  *   max_group_rows, max_shared: upper bounds of a group's rows and shared pages; what
  *     a group shares beyond max_shared is read through the own tables, and a group of
- *     more rows than max_group_rows shares nothing.
+ *     more rows than max_group_rows shares nothing.  The work is cut up by the bounds
+ *     (where max_shared covers max_length, as if either kind of page were all of it).
  * All else as tss_window_attn: q, out, row_offsets, lengths, max_rows, max_length,
  * scale, rows that see nothing, the cache's contents, and the workspace, of
  * tss_prefix_attn_bytes() bytes.  Paper: Problem Formulation (several continuations of

@@ -266,7 +266,8 @@ def prefix_attention(q, pages, page_table, row_offsets, lengths, shared, group_o
     shared: int32 [groups], how many first entries of the page tables of a group's sequences name the same pages.
     group_offsets: int32 [groups + 1], a group's first sequences; None for one group of all (then shared has one entry).
     max_shared and max_group_rows: upper bounds of a group's shared pages and rows (without them the page table's and
-    all of q's; tighter bounds launch less).  The other arguments are window_attention's."""
+    all of q's).  The work is cut up by the bounds, so tight ones, max_rows and max_length too, take less time.  The
+    other arguments are window_attention's."""
     kv = _cache(pages, page_table)
     dev = pages.device
     rows, heads, out, q_stride, out_stride, scale = _queries(kv, q, pages, scale, out)

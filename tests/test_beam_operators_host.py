@@ -94,6 +94,27 @@ def test_prefix_of_nothing_and_workspace():
     assert abi.tss_prefix_attn_bytes(cache(), 7, **sizes) == 0
 
 
+@pytest.mark.parametrize("kind", [abi.TSS_T_F16, abi.TSS_T_F32])
+@pytest.mark.parametrize("rows,length", [(2, 32768), (2, 20000), (8, 32768), (3, 4096)])
+def test_prefix_bounds_that_say_nothing(kind, rows, length):
+    """The workspace holds a state of each row and head for every split.  Where max_shared covers the longest walk, as it
+    does without bounds, the sequences' own pages are cut up as they are without a group."""
+    kv = cache(n_kv_heads=32, head_dim=128, type=kind, n_seqs=rows, table_stride=2048, n_pages=1 << 16)
+
+    def states(groups, shared):
+        need = abi.tss_prefix_attn_bytes(kv, 32, rows, 1, length, groups, rows, shared)
+        state = rows * 32 * (128 + 2) * 4
+        assert need % state == 0
+        return need // state or 1
+
+    pages = length // 16
+    alone, tight = states(0, 0), states(1, pages - 1)   # tight: one of the states is that of the one page left
+    assert alone > 1 and tight > 1
+    for shared in (pages, pages + 1, 2048):
+        # a page more in the shared walk may take one split more or less
+        assert states(1, shared) >= tight - 1 + alone - 1
+
+
 @pytest.mark.parametrize("bad", [
     dict(type=3), dict(n_groups=-1), dict(n_beams=0), dict(n_beams=33), dict(vocab=0), dict(row_stride=99),
     dict(n=0), dict(n=65, n_beams=32), dict(vocab=1, row_stride=1, n=4), dict(end_token=-1), dict(end_token=100),

@@ -186,6 +186,14 @@ def test_bounds(kind):
     compare(out[[3, 4, 5]], q[[3, 4, 5]], [0, 1, 2, 0], c)
 
 
+@pytest.mark.parametrize("kind", ["f16", "f32"])
+@pytest.mark.parametrize("rows", [[1, 2, 1], [3, 1, 40], [0, 1, 1]])
+def test_long_own_pages_without_bounds(rows, kind):
+    """Own pages in several splits beside those of the shared ones, where either kind is most of the walk."""
+    check([(2, [5003, 3333]), (300, [4825])], rows, 2, 2, 64, kind, seed=17)
+    check([(1, [2500, 20]), (0, [4000])], rows, 1, 4, 128, kind, seed=18)
+
+
 def test_scale_strides_layers_and_rows_behind():
     c = Groups([(2, [40, 33])], 2, 64, "f16", 6, layers=3)
     buf = torch.zeros(6, 6 * 64 + 8, dtype=torch.float16, device=DEV)
