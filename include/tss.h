@@ -372,8 +372,9 @@ int tss_seq_fork(tss_ctx* ctx, int32_t src, const int32_t* dst, int32_t n_dst, i
  * the same in all of them (forks of one prompt) and stay where they are; the pages
  * behind them are moved on the device, in place, on the context's stream (without
  * waiting; later calls are ordered behind).  TSS_EINVAL for unknown or repeated
- * sequences, more than 32, a parent outside [0, n), another `first`.  Paper: Problem
- * Formulation (several continuations of one prefix). */
+ * sequences, more than 32, a parent outside [0, n), another `first`, and where the
+ * longest parent's pages of one layer behind `first` are 32 GiB or more (one launch).
+ * Paper: Problem Formulation (several continuations of one prefix). */
 int tss_seq_reorder(tss_ctx* ctx, const int32_t* seqs, const int32_t* parents, int32_t n, int32_t first);
 
 /* The n best continuations of each group of beams, from the logits of the last
@@ -624,7 +625,8 @@ int tss_beam_select(void* hip_stream, const void* logits, int32_t type, int64_t 
  * lengths[] tokens, at most those of max_own tokens; a beam that is its own parent,
  * or whose parent is outside [0, n_beams), stays.  kv->n_seqs must be a multiple of
  * n_beams, 1 <= n_beams <= 32; parents, lengths [n_seqs], shared [n_seqs / n_beams]:
- * device.  The moved pages must be each sequence's own; pages outside the
+ * device; at most 65535 groups, and less than 32 GiB of pages for max_own tokens of
+ * one layer.  The moved pages must be each sequence's own; pages outside the
  * pool are neither read nor written.  The caller moves its own lengths.  Paper:
  * Problem Formulation (the committed prefix). */
 int tss_reorder_pages(void* hip_stream, const tss_paged_kv* kv, const int32_t* parents, int32_t n_beams,

@@ -1952,7 +1952,8 @@ int tss_seq_reorder(tss_ctx* c, const int32_t* seqs, const int32_t* parents, int
       window[i] = c->window[s];
     }
     if (any && a.max_own > 0) {
-      if (!launch_reorder || !reorder_fits(a)) return fail(c, TSS_EINVAL, "built without the operators' kernels");
+      if (!launch_reorder) return fail(c, TSS_EINVAL, "built without the operators' kernels");
+      if (!reorder_fits(a)) return fail(c, TSS_EINVAL, "too many pages for one launch");
       HIPCHK(launch_reorder(a, c->stream), "reordering");
     }
     for (int i = 0; i < n; ++i) {
@@ -1978,7 +1979,8 @@ int tss_get_beams(tss_ctx* c, int32_t n_groups, int32_t n_beams, const float* sc
     return fail(c, TSS_EINVAL, "n outside [1, min(64, n_beams * vocab)]");
   if (!scores || !score || !parent || !token) return fail(c, TSS_EINVAL, "null array");
   if (ended && (end_token < 0 || end_token >= V)) return fail(c, TSS_EINVAL, "end_token outside the vocabulary");
-  if (!launch_beams || !beams_fit(n_groups, n_beams, V)) return fail(c, TSS_EINVAL, "vocabulary too large");
+  if (!launch_beams) return fail(c, TSS_EINVAL, "built without the operators' kernels");
+  if (!beams_fit(n_groups, n_beams, V)) return fail(c, TSS_EINVAL, "vocabulary too large");
   // scratch as tss_get_logprobs has it: scores and ended beams, the results, the call's own
   const size_t rows = (size_t)n_groups * n_beams, nc = (size_t)n_groups * n, words = 2 * rows + 3 * nc;
   const size_t own = align256(words * 4), need = own + beams_bytes(n_groups, n_beams, V, n);
