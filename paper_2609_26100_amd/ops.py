@@ -200,6 +200,24 @@ def _frequencies(base, head_dim):
     return (ctypes.c_double * half)(*(float(base) ** (-2.0 * j / head_dim) for j in range(half)))
 
 
+def _rotation(rope, head_dim):
+    """append_kv's rope as the library takes it."""
+    if rope is None:
+        return None
+    if not hasattr(rope, "__len__") or getattr(rope, "ndim", 1) == 0:      # a number, or an array of one without axes
+        rope = float(rope)
+        if not 0 < rope < float("inf"):
+            raise ValueError("the rotation's base must be positive and finite")
+        try:
+            return _frequencies(rope, head_dim)
+        except OverflowError:
+            raise ValueError("the rotation's base is too small: its frequencies exceed float64") from None
+    freq = [float(x) for x in rope]
+    if len(freq) != head_dim // 2:
+        raise ValueError("rope must have head_dim / 2 frequencies")
+    return (ctypes.c_double * len(freq))(*freq)
+
+
 def append_kv(q, k, v, pages, page_table, row_offsets, lengths, positions=None, rope=10000.0, layer=0, max_rows=None,
               out=None):
     """Appends rows to one layer of the cache, rotated to their positions, and returns their rotated queries: row i of
@@ -241,18 +259,7 @@ def append_kv(q, k, v, pages, page_table, row_offsets, lengths, positions=None, 
             q_at, q_out, q_stride = q.data_ptr(), out.data_ptr(), _by_heads(q, "q", q_shape)
     offs, lens, max_rows, _ = _sequences(kv, row_offsets, lengths, rows, max_rows, None, dev)
     pos = None if positions is None else _indices(positions, "positions", (rows,), dev)
-    if rope is None:
-        freq = None
-    elif not hasattr(rope, "__len__"):
-        rope = float(rope)
-        if not 0 < rope < float("inf"):
-            raise ValueError("the rotation's base must be positive and finite")
-        freq = _frequencies(rope, hd)
-    else:
-        freq = [float(x) for x in rope]
-        if len(freq) != hd // 2:
-            raise ValueError("rope must have head_dim / 2 frequencies")
-        freq = (ctypes.c_double * len(freq))(*freq)
+    freq = _rotation(rope, hd)
     _call(dev, abi.tss_append_kv, kv, layer, q_at, q_stride, heads, k.data_ptr(), _by_heads(k, "k", shape), v.data_ptr(),
           _by_heads(v, "v", shape), _TYPES[dtype], offs, lens, pos, rows, max_rows, freq, q_out, out_stride)
     return out

@@ -182,3 +182,17 @@ def test_tensors_off_the_gpu_are_refused():
 def test_frequencies():
     f = ops._frequencies(10000.0, 128)
     assert len(f) == 64 and f[0] == 1.0 and abs(f[32] - 0.01) < 1e-17 and f is ops._frequencies(10000.0, 128)
+
+
+def test_rotations_refused():
+    for rope in (0.0, -1.0, float("inf"), float("nan"), 5e-324, [1.0] * 63, [1.0] * 65, []):
+        with pytest.raises(ValueError):
+            ops._rotation(rope, 128)
+    assert ops._rotation(None, 64) is None
+
+
+def test_rotations_of_every_kind_of_number():
+    want = list(ops._frequencies(500000.0, 64))
+    for rope in (500000, 500000.0, torch.tensor(500000.0), torch.tensor(500000.0).numpy(), want,
+                 torch.tensor(want, dtype=torch.float64)):
+        assert list(ops._rotation(rope, 64)) == want
