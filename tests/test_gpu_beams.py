@@ -50,6 +50,62 @@ def test_first_step(kind):
     assert (r.parent == 0).all()
 
 
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("vocab", [4001, 30000, 70001])
+def test_beams_whose_values_are_nearer_than_fp32_steps(vocab, kind):
+    """Logits of 0 and -inf, whose sums of exponentials are whole numbers and exact: values are off by the logarithm's and
+    two sums' roundings in 64 bits, at most 2e-14 below 64, so that scores one fp32 step of 4e-6 wide around -60, and of
+    5e-7 around a value of 0, say which of two beams is the better one."""
+    g = torch.Generator().manual_seed(vocab)
+    for level in (-60.0, 0.0):
+        left = torch.randint(vocab // 2, vocab, (64, 2), generator=g)
+        x = torch.zeros(128, vocab)
+        for i, n in enumerate(left.flatten().tolist()):
+            x[i, torch.randperm(vocab, generator=g)[n:]] = -torch.inf
+        scores = (level + left.double().log()).float()
+        want = scores.double() - left.double().log()
+        best = want.max(1)
+        gap = (want[:, 0] - want[:, 1]).abs()
+        assert (gap > 1e-12).all() and (gap < 8e-6).all()        # of the inputs: no tie, and none that fp32 would tell
+        x = x.to(ref.TYPES[kind])
+        r = ops.beam_select(x.to(DEV), scores.to(DEV), 1)
+        assert torch.equal(r.parent[:, 0].cpu().long(), best.indices)
+        err = (r.score[:, 0].cpu().double() - best.values).abs()
+        assert (err <= 2e-14 + ref.F32 * best.values.abs()).all()
+    few = torch.randint(1, 8, (3, 16), generator=g)              # beams of up to 7 tokens: each of them in its place
+    x = torch.full((48, vocab), -torch.inf)
+    for i, n in enumerate(few.flatten().tolist()):
+        x[i, torch.randperm(vocab, generator=g)[:n]] = 0.0
+    scores = (-60 + few.double().log()).float()
+    r = ops.beam_select(x.to(ref.TYPES[kind]).to(DEV), scores.to(DEV), 64)
+    for i in range(3):
+        v = ref.candidates(x[16 * i:16 * i + 16].numpy(), scores[i].numpy())
+        _, parent, token = ref.select(v, 64)
+        n = int(few[i].sum().clamp_max(64))
+        assert r.parent[i, :n].tolist() == parent[:n].tolist() and r.token[i, :n].tolist() == token[:n].tolist()
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("vocab", [37, 1000, 32000, 131072])
+@pytest.mark.parametrize("spread", [0.3, 2.0, 5.0])
+def test_values_near_zero(spread, vocab, kind):
+    """Scores that leave a best token's value near 0, where fp32 has small steps, show what the sums are off by.  Of an
+    exponential: the roundings of x - m, of its product with log2 e and of the sum with the product's rest, 2^-24 of the
+    argument each, and one step, 2^-23; of eight of them added in fp32 seven roundings of 2^-24.  The rest is in 64 bits."""
+    x, _ = make(24, 1, vocab, kind, vocab, spread)
+    z = x.double()
+    m = z.max(1, keepdim=True).values
+    e = (z - m).exp()
+    total = e.sum(1)
+    depth = (e * (m - z)).sum(1) / total                         # mean size of the arguments
+    scores = total.log().float()
+    want = scores.double() - total.log()
+    r = ops.beam_select(x.to(DEV), scores[:, None].contiguous().to(DEV), 1)
+    assert torch.equal(r.token[:, 0].cpu().long(), z.argmax(1))
+    err = (r.score[:, 0].cpu().double() - want).abs()
+    assert (err <= (3 * depth + 9) * 2.0 ** -24 * 1.001 + 1e-13).all(), (err.max(), depth)
+
+
 def few_left(beams, vocab, kind, which):
     """Beams few of which can go on, or whose best candidates lie in few places: (x, scores, ended)."""
     x, scores = make(2, beams, vocab, kind, beams + vocab)
