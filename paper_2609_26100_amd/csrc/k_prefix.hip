@@ -261,8 +261,11 @@ hipError_t launch_typed(const PrefixArgs& a, float* ws, hipStream_t s) {
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || n == 1) return e;
+  // as behind the windows' kernels, by waves only after blocks of many rows (four beams behind 1008
+  // tokens of 32 heads, a call in a graph, 14.4 us by workgroups, 14.7 by waves; 8 behind 4000 24.0
+  // and 24.3)
   if constexpr (sizeof(T) == 2)
-    if (n <= kWaveSplits) {
+    if (n <= kWaveSplits && p.shared.body + p.own.body > 0) {
       TSS_LAUNCH((k_window_join_wave<HD, PrefixArgs>), dim3(a.max_rows, a.n_seqs, (heads + 3) / 4), dim3(256), 0, s, a,
                  n, part_o, part_ml);
       return hipGetLastError();
