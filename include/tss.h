@@ -544,7 +544,8 @@ int tss_copy_pages(void* hip_stream, const tss_paged_kv* kv, const int32_t* src,
  * sequence of r rows (rows and lengths as tss_window_attn has them, so lengths
  * count the new rows) is the token of slot p = lengths[s] - r + i.  Its K goes
  * rotated and its V as it is to that slot, its queries rotated to q_out, ready
- * for tss_window_attn or tss_prefix_attn.
+ * for tss_window_attn or tss_prefix_attn (to which a row sees every slot up to its own:
+ * the nodes of a tree, whose siblings must not see each other, need another attention).
  *   q [rows][n_q_heads][head_dim], k, v [rows][n_kv_heads][head_dim] of `type`,
  *     rows their stride apart (elements, multiples of 8: parts of one projection's
  *     output, for instance), aligned to 16 bytes.  n_q_heads is any number; 0 with

@@ -146,7 +146,8 @@ def beam_decode(verifier, seq, root, max_new, beams, end_token=None):
 
     beams: sequences of the verifier, other than seq, whose contents may be replaced, one for each beam, at most
     max_batch.  They take seq's skip mask and window; seq itself stays as it is.  A score of -inf is no continuation
-    (fewer tokens with a finite logit than beams)."""
+    (fewer tokens with a finite logit than beams).  What the beams' sequences hold afterwards is not the returned tokens
+    (the last step is neither committed nor reordered): to go on, fork seq again and prefill those."""
     beams = [int(s) for s in abi._int32s(beams, "beams")]
     n = len(beams)
     if not 1 <= n <= min(verifier.cfg.max_batch, abi.TSS_BEAMS_MAX) or len(set(beams)) < n or seq in beams:

@@ -225,10 +225,11 @@ def append_kv(q, k, v, pages, page_table, row_offsets, lengths, positions=None, 
 
     q: [rows][any heads][head_dim] (None: keys and values alone, returns None), k, v: [rows][the cache's
     heads][head_dim], all of one type, float32, float16 or bfloat16; rows may be apart, as parts of one projection's
-    output are.  positions: int32 [rows], for rows whose position is not their slot (a tree's nodes).  rope: the
-    rotation's base, or its head_dim / 2 frequencies (host numbers), or None for no rotation.  max_rows: upper bound of
-    a sequence's rows.  out: the rotated queries, of the cache's type; may be q, otherwise shares no element with an
-    input.  Rows behind the last sequence and before token 0 are left as they were."""
+    output are.  positions: int32 [rows], for rows whose position is not their slot (a tree's nodes, which the attentions
+    here do not keep from seeing their siblings).  rope: the rotation's base, or its head_dim / 2 frequencies (host
+    numbers), or None for no rotation.  max_rows: upper bound of a sequence's rows.  out: the rotated queries, of the
+    cache's type; may be q, otherwise shares no element with an input.  Rows behind the last sequence and before token 0
+    are left as they were."""
     kv = _cache(pages, page_table)
     dev, hd = pages.device, kv.head_dim
     _on_device(k, "k", dev)
