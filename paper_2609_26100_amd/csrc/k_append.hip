@@ -10,8 +10,8 @@
 // dimensions of a group of four tokens, which the cache holds side by side: 16-byte
 // loads and stores, except where only some of the four are new.
 //
-// Bound by HBM for many rows (3500 rows of 40 + 2 x 40 heads of 128, fp32 to fp16, 323 MB: 60 us,
-// 5.3 TB/s), by a launch and three dependent loads for few (one row of 32 + 2 x 32 heads 5.2 us).
+// Bound by HBM for many rows (3500 rows of 40 + 2 x 40 heads of 128, fp32 to fp16, 323 MB: 65.5 us,
+// 4.9 TB/s), by a launch and three dependent loads for few (one row of 32 + 2 x 32 heads 5.7 us).
 #include "../../include/tss.h"
 #include "tss_internal.h"
 
@@ -183,8 +183,8 @@ template <typename T, int HD, int TYPE>
 hipError_t launch_typed(const AppendArgs& a, hipStream_t s) {
   const int all = a.n_q_heads + 2 * a.n_heads, tokens = std::min(a.max_rows, kPage);
   const int blocks = (a.max_rows + 14) / kPage + 1;
-  // two items a thread: one row of 96 heads takes 5.2 us (four: 6.9), 500 rows of 48 8.2 (one: 8.7),
-  // 3500 rows of 120 60 (one: 64, four: 65)
+  // two items a thread: one row of 96 heads takes 5.6 us (one: 5.7, four: 7.3), 3500 rows of 120 65.4
+  // (67, 72); 500 rows of 48 6.9 (6.2, 7.3)
   const int units = std::max(1, kAppendThreads * 2 / (HD / 16 * tokens));
   const dim3 grid(blocks, a.n_seqs, (all + units - 1) / units);
   TSS_LAUNCH((k_append<T, HD, TYPE>), grid, dim3(kAppendThreads), 0, s, a, units);

@@ -17,8 +17,8 @@
 // the group (16 beams of 32000 equal logits 1.3 ms).
 //
 // Bound by HBM where there is much to read (32 groups of 16 beams of 131072 bf16 logits, 134 MB:
-// the first launch 24 us, 5.6 TB/s; the second 14, on 32 CUs), else by the dependent
-// phases of two launches (four beams of 32000 fp32: 3.9 + 8.2 us, of which the second's
+// the first launch 24 us, 5.6 TB/s; the second 13.5, on 32 CUs), else by the dependent
+// phases of two launches (four beams of 32000 fp32: 3.8 + 8.3 us, of which the second's
 // sums take 1.6, its cut 3, what is opened 2.1 and the order 0.7).
 //
 // Values are (x - m) + c in 64 bits, c the score less the logarithm.  In S, 8 exponentials

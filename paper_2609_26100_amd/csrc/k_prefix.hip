@@ -5,15 +5,15 @@
 // window_core.h, whose states (maximum, sum, outputs) say all about a part of the
 // tokens), a second joins a row's states.  The blocks of the shared pages hold the rows of
 // the whole group beside each other, so that a page is read once for all of them (once
-// for every 128 virtual rows); they need no masks.
+// for every 128 virtual rows, of an fp32 cache for every 16); they need no masks.
 //
 // Bound by HBM where the own pages weigh most (64 sequences of 32 heads, 300 own tokens behind
-// 8000 shared ones, 446 MB: 97 us, 4.6 TB/s) or a group has few rows (8 sequences of 32
-// heads over 8 kv heads behind 16000 tokens, 72 MB: 21 us); by the blocks' steps, as in
+// 8000 shared ones, 446 MB: 92 + 5 us, 4.9 TB/s) or a group has few rows (8 sequences of 32
+// heads over 8 kv heads behind 16000 tokens, 66 MB: 16 + 4 us); by the blocks' steps, as in
 // k_window.hip, where a page serves many rows (64 of 4 heads a kv head behind 32000 tokens:
 // 69 + 7 us, 450 TFLOP/s); by two launches and the walk from the group to its pages
 // (five loads one behind the other) where all is short (four beams behind 1008 tokens
-// 8.7 + 3.5 us).
+// 9.0 + 3.9 us).
 //
 // A row that stands inside the shared pages cuts them down for its group, to the pages
 // that every row sees whole; the rest is read through the sequences' own tables.  Every
