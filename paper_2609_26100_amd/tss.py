@@ -425,7 +425,7 @@ def tss_get_beams(ctx, scores, n, ended=None, end_token=0):
     e = None if ended is None else _int32s(ended, "ended")
     if e is not None and e.shape != s.shape:
         raise ValueError("ended must be like scores")
-    shape = (s.shape[0], max(n, 0))
+    shape = (s.shape[0], min(max(n, 0), TSS_BEAMS_MAX_N))        # the library refuses other numbers
     score, parent, token = np.empty(shape, np.float32), np.empty(shape, np.int32), np.empty(shape, np.int32)
     _check(lib().tss_get_beams(ctx, s.shape[0], s.shape[1], _ptr(s), _ptr(e), end_token, n, _ptr(score), _ptr(parent),
                                _ptr(token)), ctx, "tss_get_beams")

@@ -166,6 +166,13 @@ def test_numbers_that_do_not_fit():
                     call(**{name: x})
 
 
+@pytest.mark.parametrize("n", [0, -1, 65, (1 << 31) - 1])
+def test_numbers_of_beams_refused_by_the_library(n):
+    """Without a context the library refuses every call: no room is made first for more results than there can be."""
+    with pytest.raises(abi.TSSError):
+        abi.tss_get_beams(None, torch.zeros(100000, 2).numpy(), n)
+
+
 def test_tensors_off_the_gpu_are_refused():
     pages, x = torch.zeros(1, 2, 2, 1, 16 * 64), torch.zeros(1, 1, 64)
     i = torch.zeros(1, 1, dtype=torch.int32)
