@@ -87,6 +87,20 @@ def test_one_beam_is_greedy_decoding(models):
     assert abs(r.scores[0] - want.logprobs.logprob.sum()) < 1e-3
 
 
+def test_nothing_cached_before_the_root(models):
+    v, _ = models("f32")
+    for q in range(4):
+        v.truncate(q, 0)
+        v.set_window(q, 0, 0)
+        v.set_mask(q, None)
+    r = beam_decode(v, 0, 7, 20, [3])
+    want = autoregressive_decode(v, 0, 7, 20)
+    np.testing.assert_array_equal(r.tokens[0], want.tokens)
+    v.truncate(0, 0)
+    three = beam_decode(v, 0, 7, 20, [1, 2, 3])
+    assert (np.diff(three.scores) <= 0).all() and len(three.tokens[0]) == 20 and v.length(0) == 0
+
+
 def test_ended_beams(models):
     """A beam that ends keeps its score, and the search stops when all have ended."""
     v, _ = models("f32")
