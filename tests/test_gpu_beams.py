@@ -139,21 +139,23 @@ def test_few_beams_that_can_go_on(which, beams, vocab, n, kind):
 
 
 def replays_us(f, n=20):
+    """The shortest of some replays of a captured call, of three graphs: now and then all of one take longer."""
     f()
     torch.cuda.synchronize()
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
-        f()
     times = []
-    for _ in range(7):
-        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-        graph.replay()
-        a.record()
-        for _ in range(n):
+    for _ in range(3):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            f()
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
             graph.replay()
-        b.record()
-        torch.cuda.synchronize()
-        times.append(a.elapsed_time(b) * 1000 / n)
+            a.record()
+            for _ in range(n):
+                graph.replay()
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b) * 1000 / n)
     return min(times)
 
 
